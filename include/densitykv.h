@@ -12,7 +12,11 @@
  *                             request, every bank state's density (Eq. 3);
  *   densitykv_update_bank     the full update of Algorithm 1 for all banks;
  *   densitykv_bank_attention  softmax(q k^T * scale) v over [bank; window];
- *   densitykv_bank_attention_sink  the same over [bank; window; sink].
+ *   densitykv_bank_attention_sink  the same over [bank; window; sink];
+ *   densitykv_cache_write, densitykv_cache_read, densitykv_cache_attention
+ *                             the local window and the first tokens held in
+ *                             pages (8 or 4 bits a value on request): rows
+ *                             written, read back, and attended with the bank.
  *
  * Conventions shared by every entry point
  *   - Every pointer inside the structs and every array argument is DEVICE
@@ -352,6 +356,131 @@ int densitykv_bank_attention_ws(const dkv_bank *bank, const void *q, int32_t n_q
  */
 int densitykv_pair_weight_q23(const float *d2, int64_t n, const dkv_params *prm,
                               int32_t *w_q23, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged window cache: the tokens of the local window, and first tokens that stay
+ * visible, of several sequences in pages of one pool.  A generation loop writes
+ * the new tokens' rows (densitykv_cache_write), lets their queries read
+ * [bank; cache] (densitykv_cache_attention), and hands the block that leaves the
+ * window to densitykv_update_bank (densitykv_cache_read gives it as a segment).
+ *
+ * Formats of a row of d elements in a page:
+ *   DKV_CACHE_FULL  the elements in `dtype`;
+ *   DKV_CACHE_FP8   d bytes, OCP e4m3 (largest value F = 448);
+ *   DKV_CACHE_FP4   d / 2 bytes, OCP e2m1 (F = 6), element 2 i in the low half
+ *                   of byte i.
+ * FP8 and FP4 rows have one scale for each 32 elements, a power of two held as
+ * its exponent + 127 in one byte.  Writing takes the smallest exponent e >= -100
+ * with max |x| <= F 2^e (so nothing saturates) and stores x 2^-e rounded to
+ * nearest, ties to even: an element is off by at most 2^-4 (FP8) or 2^-2 (FP4) of
+ * its value, or half the smallest step (2^-10, 2^-2) times 2^e where that is
+ * more.  A group that holds a NaN or an infinity gets the scale byte 255 and
+ * reads back as NaN throughout.  What a row stands for is exact in bf16, so
+ * every reader sees the same values. */
+typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_cache_format;
+
+/*
+ *   k, v             [P, H, page_size, row bytes]   16-byte aligned
+ *   k_scale, v_scale [P, H, page_size, d / 32]      NULL for DKV_CACHE_FULL
+ *   page_table       [S, max_pages] int32           page of the tokens page_size i ..
+ *                    of a sequence; an entry outside [0, P) is an absent page: its
+ *                    tokens are not written, read as zeros and are not attended
+ *   length           [S] int32   tokens of each sequence, the new ones of a chunk
+ *                    included; clamped on the device to [0, max_pages * page_size]
+ * Rows at or behind the length, and pages that no visible token lies in, may hold
+ * anything.  A page may belong to several sequences as long as no call writes to
+ * it for more than one of them.
+ */
+typedef struct {
+  int32_t num_seqs;     /* S >= 1 */
+  int32_t num_kv_heads; /* H >= 1 */
+  int32_t head_dim;     /* 64 or 128 */
+  int32_t page_size;    /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t num_pages;    /* P >= 1 */
+  int32_t max_pages;    /* row length of page_table; max_pages * page_size <= 2^30 */
+  int32_t dtype;        /* dkv_dtype of the rows written and read and of the queries */
+  int32_t format;       /* dkv_cache_format */
+  void *k;
+  void *v;
+  uint8_t *k_scale;
+  uint8_t *v_scale;
+  const int32_t *page_table;
+  const int32_t *length;
+} dkv_cache;
+
+/* The new tokens of all sequences, packed: sequence s has the rows start[s] ..
+ * start[s + 1] of a call's arrays, and they are its last tokens: row start[s] + i
+ * is position length[s] - n_s + i, n_s = start[s + 1] - start[s].
+ *   n_tokens  T, rows of the arrays (0..2^24); start is clamped on the device to
+ *             [0, T], rows behind the last sequence's are neither read nor written
+ *   max_new   an upper bound of every n_s (it sizes the launch): rows of a sequence
+ *             beyond its first max_new are neither read nor written
+ *   start     [S + 1] int32 ascending, or NULL: T / S tokens each (T divisible by S)
+ */
+typedef struct {
+  int32_t n_tokens;
+  int32_t max_new;
+  const int32_t *start;
+} dkv_chunk;
+
+/*
+ * Write the chunk's rows into their pages.  k, v: [T, H, d] in the cache's dtype;
+ * row t of head h starts at element t * token_stride + h * head_stride (both
+ * multiples of 16 bytes, pointers 16-byte aligned).  Rows at positions below 0 or
+ * in absent pages are dropped.
+ */
+int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, const void *v,
+                          int64_t token_stride, int64_t head_stride, void *stream);
+
+/*
+ * Read the rows of the positions first[s] .. first[s] + n of every sequence (first
+ * NULL: 0) into k, v: [S * H, n, d] in the cache's dtype, bank s * H + h the rows of
+ * head h: the layout of a dkv_segment of S * H banks.  Rows outside the sequence
+ * or in absent pages are zeros.  k and v are 16-byte aligned; n in 0..2^24.
+ */
+int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n, void *k, void *v, void *stream);
+
+/* The queries of a densitykv_cache_attention call: [T, num_heads, d] in the cache's
+ * dtype, row t of head h at element t * q_token_stride + h * q_head_stride; the
+ * output likewise (strides multiples of 16 bytes, pointers 16-byte aligned).
+ * Query head h reads the rows of head h / (num_heads / H).
+ *   causal     nonzero: a query sees the tokens up to its own position; 0: every
+ *              query of a chunk stands at the sequence's last position and sees the
+ *              whole chunk
+ *   window     W > 0: of those the W last and the sequence's n_sink first tokens;
+ *              0: all of them
+ */
+typedef struct {
+  int32_t num_heads; /* a multiple of num_kv_heads, T * num_heads < 2^31 */
+  int32_t window;    /* 0..2^30 */
+  int32_t n_sink;    /* 0..2^30 */
+  int32_t causal;
+  float softmax_scale;
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+} dkv_cache_queries;
+
+/*
+ * out = softmax(q K^T * softmax_scale) V over the visible tokens of the query's
+ * sequence and, with a bank (NULL: none), all live slots of bank s * H + h (S * H
+ * banks of the cache's head_dim and dtype).  fp32 softmax and sums; in bf16 the
+ * softmax weights are rounded to bf16 for the product with V and summed as rounded.
+ * A query that sees nothing gives zeros.  Tokens that a query does not see do not
+ * change its result, whatever they hold (NaN and infinities included).
+ *
+ * densitykv_cache_attention_workspace_size gives the bytes of device workspace
+ * that a call uses to split its keys over workgroups (0: it does not split;
+ * host-only).  With a NULL, smaller or misaligned (16 bytes) workspace the call
+ * runs unsplit.  The splits follow from the sizes alone, so equal calls give equal
+ * bits; calls that overlap in time need workspaces of their own.
+ */
+int densitykv_cache_attention_workspace_size(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank,
+                                             const dkv_cache_queries *qs, size_t *bytes);
+int densitykv_cache_attention(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank,
+                              const dkv_cache_queries *qs, const void *q, void *out, void *workspace,
+                              size_t workspace_bytes, void *stream);
 
 /* Static text for a dkv_status value. */
 const char *densitykv_status_string(int status);

@@ -13,6 +13,16 @@ Typical use (bf16 banks, one layer of 12 heads sharing the admitted prefix):
     update_bank(bank, seg_k, seg_v, block_id, prm, workspace=ws, out=out)
     o = bank_attention(bank, q, win_k, win_v)        # queries over bank + window
 
+A local window held in pages (rows in the dtype, or in 8 or 4 bits with a scale for
+each 32 elements), for sequences of different lengths:
+
+    cache = PagedCache(seqs, kv_heads, 128, num_pages, max_pages, page_size=64, format="fp8")
+    cache.page_table[s, i] = page                    # int32; the program owns the pages
+    cache.length += new_tokens                       # tokens of each sequence, the new ones included
+    cache_write(cache, k, v, start)                  # new rows [T, kv_heads, d], packed
+    o = cache_attention(cache, q, start, bank=bank, window=9360, n_sink=1560)
+    seg_k, seg_v = cache_read(cache, n, first)       # the block that leaves, as update_bank takes it
+
 Policy variants are Params.flags bits (POLICY_*); the sequential competition
 needs the larger workspace that alloc_workspace(bank, n, flags) sizes.
 """
@@ -30,6 +40,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdensitykv.so")
 
 DKV_BF16, DKV_F32 = 0, 1
+CACHE_FORMATS = {"full": 0, "fp8": 1, "fp4": 2}  # dkv_cache_format
 MAX_CANDIDATES, MAX_CAPACITY, MAX_BLOCK_ID = 8191, 32767, 16777215
 # dkv_params.flags: policy ablations of Table 1(b) (0 = the paper's policy)
 POLICY_SOURCE_ORDER = 0x1   # prefixes in source order instead of score order
@@ -46,7 +57,9 @@ SEQ_WEIGHT_BYTES = 32 << 30     # pairwise-weight bytes the sequential workspace
 ENTRY_POINTS = ("densitykv_workspace_size", "densitykv_workspace_size_policy", "densitykv_score",
                 "densitykv_update_bank", "densitykv_update_bank_noalloc",
                 "densitykv_bank_attention", "densitykv_bank_attention_sink", "densitykv_attention_workspace_size",
-                "densitykv_bank_attention_ws", "densitykv_pair_weight_q23", "densitykv_status_string")
+                "densitykv_bank_attention_ws", "densitykv_cache_write", "densitykv_cache_read",
+                "densitykv_cache_attention_workspace_size", "densitykv_cache_attention", "densitykv_pair_weight_q23",
+                "densitykv_status_string")
 
 _vp = ctypes.c_void_p
 
@@ -71,6 +84,24 @@ class DkvUpdateOut(ctypes.Structure):
     _fields_ = [("r_star", _vp), ("n_admitted", _vp), ("n_evicted", _vp), ("admitted", _vp),
                 ("evicted", _vp), ("order", _vp), ("score_q", _vp), ("first_cross", _vp),
                 ("rho_tilde", _vp)]
+
+
+class DkvCache(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("format", ctypes.c_int32), ("k", _vp), ("v", _vp), ("k_scale", _vp),
+                ("v_scale", _vp), ("page_table", _vp), ("length", _vp)]
+
+
+class DkvChunk(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32), ("start", _vp)]
+
+
+class DkvCacheQueries(ctypes.Structure):
+    _fields_ = [("num_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("n_sink", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("softmax_scale", ctypes.c_float), ("q_token_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out_token_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -101,6 +132,12 @@ def lib() -> ctypes.CDLL:
                                                          P(ctypes.c_size_t)]
         L.densitykv_bank_attention_ws.argtypes = L.densitykv_bank_attention_sink.argtypes[:-1] + [_vp, ctypes.c_size_t,
                                                                                                   _vp]
+        L.densitykv_cache_write.argtypes = [P(DkvCache), P(DkvChunk), _vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp]
+        L.densitykv_cache_read.argtypes = [P(DkvCache), _vp, ctypes.c_int32, _vp, _vp, _vp]
+        L.densitykv_cache_attention_workspace_size.argtypes = [P(DkvCache), P(DkvChunk), P(DkvBank), P(DkvCacheQueries),
+                                                               P(ctypes.c_size_t)]
+        L.densitykv_cache_attention.argtypes = [P(DkvCache), P(DkvChunk), P(DkvBank), P(DkvCacheQueries), _vp, _vp, _vp,
+                                                ctypes.c_size_t, _vp]
         L.densitykv_pair_weight_q23.argtypes = [_vp, ctypes.c_int64, P(DkvParams), _vp, _vp]
         L.densitykv_status_string.argtypes = [ctypes.c_int]
         L.densitykv_status_string.restype = ctypes.c_char_p
@@ -396,6 +433,144 @@ def bank_attention_sink(bank: Bank, q: torch.Tensor, sink_k: Optional[torch.Tens
     ns = _kv_segment(bank, sink_k, sink_v, "sink")
     nw = _kv_segment(bank, win_k, win_v, "window")
     return _attention(bank, q, nq, sink_k, sink_v, ns, win_k, win_v, nw, softmax_scale, out, "bank_attention_sink")
+
+
+class PagedCache:
+    """The paged window cache of `num_seqs` sequences (dkv_cache): the pool of pages and the
+    sequences' page tables (-1: absent) and lengths, which the program keeps up to date.
+
+    k, v: [num_pages, num_kv_heads, page_size, d] in `dtype` (format "full"), or the codes as uint8
+    ("fp8": d bytes a row, "fp4": d / 2) with k_scale, v_scale [num_pages, num_kv_heads, page_size, d / 32]."""
+
+    def __init__(self, num_seqs: int, num_kv_heads: int, head_dim: int, num_pages: int, max_pages: int,
+                 page_size: int = 64, dtype=torch.bfloat16, format: str = "full", device="cuda"):
+        if format not in CACHE_FORMATS:
+            raise ValueError(f"format must be one of {tuple(CACHE_FORMATS)}")
+        _dtype_code(dtype)
+        self.S, self.H, self.d, self.P, self.cols = num_seqs, num_kv_heads, head_dim, num_pages, max_pages
+        self.page_size, self.dtype, self.format = page_size, dtype, format
+        dev = torch.device(device)
+        full = format == "full"
+        width = head_dim if format != "fp4" else head_dim // 2
+        rows = (num_pages, num_kv_heads, page_size)
+        self.k, self.v = (torch.zeros(*rows, width, dtype=dtype if full else torch.uint8, device=dev) for _ in range(2))
+        self.k_scale, self.v_scale = (None if full else torch.zeros(*rows, head_dim // 32, dtype=torch.uint8, device=dev)
+                                      for _ in range(2))
+        self.page_table = torch.full((num_seqs, max_pages), -1, dtype=torch.int32, device=dev)
+        self.length = torch.zeros(num_seqs, dtype=torch.int32, device=dev)
+        self._c = DkvCache(num_seqs, num_kv_heads, head_dim, page_size, num_pages, max_pages, _dtype_code(dtype),
+                           CACHE_FORMATS[format], self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale),
+                           _ptr(self.v_scale), self.page_table.data_ptr(), self.length.data_ptr())
+
+    def __setattr__(self, name, value):  # kernels hold the tensors' addresses: new contents are copied into them
+        if "_c" in self.__dict__ and value is not self.__dict__.get(name):
+            raise AttributeError(f"PagedCache.{name} stays the same object: write into it")
+        object.__setattr__(self, name, value)
+
+    def c(self) -> DkvCache:
+        if not self.k.is_cuda:
+            raise ValueError("the cache's tensors are not on a GPU")
+        return self._c
+
+
+def _i32(x, what: str) -> int:
+    """An integer that the C structures hold in 32 bits (ctypes would cut it off)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{what} is out of range")
+    return x
+
+
+def _chunk(cache: PagedCache, T: int, start: Optional[torch.Tensor], max_new: Optional[int]) -> DkvChunk:
+    if start is None:
+        if T % cache.S != 0:
+            raise ValueError("without start, the tokens must divide evenly over the sequences")
+    elif (start.dtype != torch.int32 or start.shape != (cache.S + 1,) or not start.is_contiguous()
+          or start.device != cache.k.device):
+        raise ValueError("start must be a contiguous int32 [num_seqs + 1] tensor on the cache's device")
+    T = _i32(T, "the number of tokens")
+    return DkvChunk(T, T if max_new is None else _i32(max_new, "max_new"), _ptr(start))
+
+
+def _check_rows(cache: PagedCache, t: torch.Tensor, what: str):
+    """[T, heads, d] in the cache's dtype and on its device, unit stride within a row; the strides of a token and a head."""
+    if t.dim() != 3 or t.shape[2] != cache.d or t.dtype != cache.dtype or t.device != cache.k.device:
+        raise ValueError(f"{what} must be [tokens, heads, head_dim] in the cache's dtype, on its device")
+    st = t.stride()
+    if st[2] != 1 or (st[0] | st[1]) % (16 // t.element_size()) or t.data_ptr() % 16:
+        raise ValueError(f"the rows of {what} must be contiguous and start at multiples of 16 bytes")
+    return st[0], st[1]
+
+
+def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
+                max_new: Optional[int] = None):
+    """densitykv_cache_write: the new rows k, v [T, num_kv_heads, d] into their pages, on the current stream.
+    `start` [S + 1]: first row of each sequence (None: T / S rows each); `max_new`: a bound of the rows of a sequence."""
+    st = _check_rows(cache, k, "k")
+    if k.shape[1] != cache.H or v.shape != k.shape:
+        raise ValueError("k and v must be [tokens, num_kv_heads, head_dim]")
+    if _check_rows(cache, v, "v") != st:
+        raise ValueError("k and v must have the same strides")
+    cc, ch = cache.c(), _chunk(cache, int(k.shape[0]), start, max_new)
+    with torch.cuda.device(cache.k.device):
+        _check(lib().densitykv_cache_write(ctypes.byref(cc), ctypes.byref(ch), _ptr(k), _ptr(v), st[0], st[1], _stream()),
+               "cache_write")
+
+
+def cache_read(cache: PagedCache, n: int, first: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
+               v: Optional[torch.Tensor] = None):
+    """densitykv_cache_read: rows first[s] .. first[s] + n of every sequence as (k, v) [S * num_kv_heads, n, d]."""
+    if first is not None and (first.dtype != torch.int32 or first.shape != (cache.S,) or not first.is_contiguous()
+                              or first.device != cache.k.device):
+        raise ValueError("first must be a contiguous int32 [num_seqs] tensor on the cache's device")
+    n = _i32(n, "n")
+    if n < 0:
+        raise ValueError("n must not be negative")
+    shape = (cache.S * cache.H, n, cache.d)
+    k, v = (torch.empty(shape, dtype=cache.dtype, device=cache.k.device) if t is None else t for t in (k, v))
+    for t in (k, v):
+        if tuple(t.shape) != shape or t.dtype != cache.dtype or not t.is_contiguous() or t.device != cache.k.device:
+            raise ValueError("k and v must be contiguous [num_seqs * num_kv_heads, n, head_dim] tensors in the cache's dtype")
+    cc = cache.c()
+    with torch.cuda.device(cache.k.device):
+        _check(lib().densitykv_cache_read(ctypes.byref(cc), _ptr(first), n, _ptr(k), _ptr(v), _stream()),
+               "cache_read")
+    return k, v
+
+
+def cache_attention(cache: PagedCache, q: torch.Tensor, start: Optional[torch.Tensor] = None,
+                    max_new: Optional[int] = None, bank: Optional[Bank] = None, window: int = 0, n_sink: int = 0,
+                    causal: bool = True, softmax_scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """densitykv_cache_attention: q [T, num_heads, d] of the new tokens over [bank; cache]; each sees (causal) the tokens
+    up to its own position, of those the last `window` (0: all) and the first `n_sink`.  The partial results of a split call
+    are in `workspace` (uint8) if it is given, else in a buffer of the caching allocator, held for the call."""
+    qt, qh = _check_rows(cache, q, "q")
+    T, nh = int(q.shape[0]), int(q.shape[1])
+    if out is None:  # a ragged chunk may leave rows without a sequence
+        out = (torch.zeros if start is not None else torch.empty)(T, nh, cache.d, dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    ot, oh = _check_rows(cache, out, "out")
+    scale = (1.0 / cache.d ** 0.5) if softmax_scale is None else float(softmax_scale)
+    if bank is not None and bank.k.device != cache.k.device:
+        raise ValueError("the bank must be on the cache's device")
+    L, cc, ch = lib(), cache.c(), _chunk(cache, T, start, max_new)
+    cq = DkvCacheQueries(nh, _i32(window, "window"), _i32(n_sink, "n_sink"), 1 if causal else 0, scale, qt, qh, ot, oh)
+    pc, pch, pq, pb = ctypes.byref(cc), ctypes.byref(ch), ctypes.byref(cq), None
+    if bank is not None:
+        cb = bank.c()
+        pb = ctypes.byref(cb)
+    size = ctypes.c_size_t(0)
+    with torch.cuda.device(cache.k.device):
+        if workspace is None:
+            _check(L.densitykv_cache_attention_workspace_size(pc, pch, pb, pq, ctypes.byref(size)), "cache_attention")
+            if size.value:
+                workspace = torch.empty(size.value, dtype=torch.uint8, device=q.device)
+        _check(L.densitykv_cache_attention(pc, pch, pb, pq, _ptr(q), _ptr(out), _ptr(workspace),
+                                           0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                           _stream()), "cache_attention")
+    return out
 
 
 def pair_weight_q23(d2: torch.Tensor, params: Params = Params()) -> torch.Tensor:

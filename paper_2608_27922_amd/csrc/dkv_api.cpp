@@ -181,6 +181,68 @@ Geom geom_of(const dkv_bank *bk, int n) {
   return g;
 }
 
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
+  if (!c) return DKV_ERR_INVALID;
+  if (c->dtype != DKV_BF16 && c->dtype != DKV_F32) return DKV_ERR_INVALID;
+  if (c->format != DKV_CACHE_FULL && c->format != DKV_CACHE_FP8 && c->format != DKV_CACHE_FP4) return DKV_ERR_INVALID;
+  if (c->head_dim != 64 && c->head_dim != 128) return DKV_ERR_UNSUPPORTED;
+  int lps = 4;
+  while (lps < 8 && (1 << lps) != c->page_size) ++lps;
+  if ((1 << lps) != c->page_size) return DKV_ERR_SHAPE;
+  if (c->num_seqs < 1 || c->num_kv_heads < 1 || c->num_pages < 1 || c->max_pages < 1) return DKV_ERR_SHAPE;
+  if (((int64_t)c->max_pages << lps) > (int64_t(1) << 30)) return DKV_ERR_SHAPE;
+  if ((int64_t)c->num_seqs * c->num_kv_heads >= (int64_t(1) << 24)) return DKV_ERR_SHAPE;
+  if (!c->k || !c->v || !c->page_table || !c->length) return DKV_ERR_INVALID;
+  if (c->format != DKV_CACHE_FULL && (!c->k_scale || !c->v_scale)) return DKV_ERR_INVALID;
+  if (!aligned16(c->k) || !aligned16(c->v)) return DKV_ERR_INVALID;
+  *out = Pages{static_cast<unsigned char *>(c->k), static_cast<unsigned char *>(c->v), c->k_scale, c->v_scale,
+               c->page_table, c->length, nullptr, c->num_seqs, c->num_kv_heads, c->num_pages, c->max_pages, lps, 0, 0};
+  if (!ch) return DKV_OK;
+  constexpr int32_t kMax = 1 << 24;
+  if (ch->n_tokens < 0 || ch->n_tokens > kMax || ch->max_new < 0) return DKV_ERR_SHAPE;
+  if (!ch->start && ch->n_tokens % c->num_seqs != 0) return DKV_ERR_SHAPE;
+  out->start = ch->start;
+  out->T = ch->n_tokens;
+  out->max_new = ch->max_new < ch->n_tokens ? ch->max_new : ch->n_tokens;
+  if ((int64_t)out->max_new * c->num_kv_heads >= (int64_t(1) << 31)) return DKV_ERR_SHAPE;
+  return DKV_OK;
+}
+
+// Strides of rows that are read 16 bytes at a time.
+bool strides_ok(int dtype, int64_t token, int64_t head) {
+  const int64_t per = dtype == DKV_BF16 ? 8 : 4;
+  return token % per == 0 && head % per == 0;
+}
+
+// Arguments of an attention over the cache, except its pointers.
+int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank, const dkv_cache_queries *qs,
+                        Pages *c, Mask *mask, BankRows *rows) {
+  if (!chunk || !qs) return DKV_ERR_INVALID;
+  int rc = check_cache(cache, chunk, c);
+  if (rc) return rc;
+  *rows = BankRows{nullptr, nullptr, nullptr, nullptr, 0};
+  if (bank) {
+    rc = check_bank(bank);
+    if (rc) return rc;
+    if (bank->head_dim != cache->head_dim || bank->dtype != cache->dtype ||
+        (int64_t)bank->num_banks != (int64_t)c->S * c->H)
+      return DKV_ERR_SHAPE;
+    *rows = BankRows{bank->k, bank->v, bank->occupancy, bank->budget, bank->capacity};
+  }
+  if (qs->num_heads < 1 || qs->num_heads % c->H != 0) return DKV_ERR_SHAPE;
+  if ((int64_t)c->T * qs->num_heads >= (int64_t(1) << 31)) return DKV_ERR_SHAPE;
+  constexpr int32_t kMax = 1 << 30;
+  if (qs->window < 0 || qs->window > kMax || qs->n_sink < 0 || qs->n_sink > kMax) return DKV_ERR_SHAPE;
+  if (!(qs->softmax_scale > 0.0f) || qs->softmax_scale > 1e6f) return DKV_ERR_RANGE;
+  if (!strides_ok(cache->dtype, qs->q_token_stride, qs->q_head_stride) ||
+      !strides_ok(cache->dtype, qs->out_token_stride, qs->out_head_stride))
+    return DKV_ERR_SHAPE;
+  *mask = Mask{qs->window, qs->window > 0 ? qs->n_sink : 0, qs->causal ? 1 : 0};
+  return DKV_OK;
+}
+
 bool attention_sizes_ok(int32_t nq, int32_t nw, int32_t ns) {
   constexpr int32_t kMax = 1 << 24;
   return nq >= 0 && nw >= 0 && ns >= 0 && nq <= kMax && nw <= kMax && ns <= kMax;
@@ -331,6 +393,62 @@ int densitykv_bank_attention(const dkv_bank *bank, const void *q, int32_t n_quer
                              void *stream) {
   return densitykv_bank_attention_sink(bank, q, n_query, nullptr, nullptr, 0, win_k, win_v, n_window, out,
                                        softmax_scale, stream);
+}
+
+int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, const void *v,
+                          int64_t token_stride, int64_t head_stride, void *stream) {
+  Pages c{};
+  if (!chunk) return DKV_ERR_INVALID;
+  int rc = check_cache(cache, chunk, &c);
+  if (rc) return rc;
+  if (!strides_ok(cache->dtype, token_stride, head_stride)) return DKV_ERR_SHAPE;
+  if (c.max_new > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
+  hipError_t e = launch_cache_write(c, cache->dtype, cache->format, cache->head_dim, k, v, token_stride, head_stride,
+                                    static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
+}
+
+int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n, void *k, void *v, void *stream) {
+  Pages c{};
+  int rc = check_cache(cache, nullptr, &c);
+  if (rc) return rc;
+  if (n < 0 || n > (1 << 24)) return DKV_ERR_SHAPE;
+  if (n > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
+  hipError_t e = launch_cache_read(c, cache->dtype, cache->format, cache->head_dim, first, n, k, v,
+                                   static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
+}
+
+int densitykv_cache_attention_workspace_size(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank,
+                                             const dkv_cache_queries *qs, size_t *bytes) {
+  Pages c{};
+  Mask mask{};
+  BankRows rows{};
+  int rc = check_cache_queries(cache, chunk, bank, qs, &c, &mask, &rows);
+  if (rc) return rc;
+  if (!bytes) return DKV_ERR_INVALID;
+  cache_attention_splits(c, cache->dtype, cache->format, cache->head_dim, mask, rows, qs->num_heads, bytes);
+  return DKV_OK;
+}
+
+int densitykv_cache_attention(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank,
+                              const dkv_cache_queries *qs, const void *q, void *out, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+  Pages c{};
+  Mask mask{};
+  BankRows rows{};
+  int rc = check_cache_queries(cache, chunk, bank, qs, &c, &mask, &rows);
+  if (rc) return rc;
+  if (c.max_new > 0 && (!q || !out || !aligned16(q) || !aligned16(out))) return DKV_ERR_INVALID;
+  if (bank && (!aligned16(bank->k) || !aligned16(bank->v))) return DKV_ERR_INVALID;
+  size_t need = 0;
+  int nsplit = cache_attention_splits(c, cache->dtype, cache->format, cache->head_dim, mask, rows, qs->num_heads, &need);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need) nsplit = 1;
+  const CacheQueries cq{q, out, qs->q_token_stride, qs->q_head_stride, qs->out_token_stride, qs->out_head_stride,
+                        qs->num_heads, qs->num_heads / c.H, qs->softmax_scale * 1.4426950408889634f};
+  hipError_t e = launch_cache_attention(c, cache->dtype, cache->format, cache->head_dim, mask, rows, cq, workspace, nsplit,
+                                        static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
 }
 
 int densitykv_pair_weight_q23(const float *d2, int64_t n, const dkv_params *prm, int32_t *w_q23,

@@ -1,0 +1,149 @@
+// Rows of the paged window cache: written (quantised on the way) and read back.
+//
+// Both are one pass over the data with 8 elements per thread: 16 bytes of a bf16 row
+// in or out, so a wave reads and writes whole 128-byte lines on both sides.  The
+// largest magnitude of a group of 32 comes from four neighbouring lanes.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "dkv_cache_format.hpp"
+
+namespace dkv {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Thread = 8 elements of one row (token, head) of K (z = 0) or V (z = 1) of sequence y.
+template <int DT, int FMT, int D>
+__global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *__restrict__ k, const void *__restrict__ v,
+                                                          int64_t ts, int64_t hs, int nb) {
+  constexpr int CH = D / 8;
+  const int z = (int)(blockIdx.x / (unsigned)nb) & 1, s = (int)(blockIdx.x / (unsigned)nb) >> 1;
+  const NewRows nr = new_rows(c, s);
+  const int ch = (int)threadIdx.x % CH;
+  const unsigned row = (blockIdx.x % (unsigned)nb) * (kThreads / CH) + threadIdx.x / CH;  // (token, head)
+  const int i = (int)(row / (unsigned)c.H), h = (int)(row % (unsigned)c.H);
+  if (i >= min(nr.n, c.max_new)) return;  // whole groups of four lanes leave together
+  const int pos = seq_length(c, s) - nr.n + i;
+  if (pos < 0) return;
+  const int p = page_of(c, s, pos);
+  if (p < 0) return;
+  const int64_t at = (int64_t)(nr.first + i) * ts + h * hs + 8 * ch;
+  const void *src = z ? v : k;
+  unsigned char *dst = z ? c.v : c.k;
+  const size_t r = pool_row(c, p, h, pos);
+  if constexpr (FMT == DKV_CACHE_FULL) {
+    constexpr int E = DT == DKV_BF16 ? 1 : 2;
+    const uint4 *x = reinterpret_cast<const uint4 *>(static_cast<const char *>(src) + at * (2 * E));
+    uint4 *o = reinterpret_cast<uint4 *>(dst + r * (2 * E * D) + 16 * E * ch);
+#pragma unroll
+    for (int j = 0; j < E; ++j) o[j] = x[j];
+  } else {
+    float x[8];
+    if constexpr (DT == DKV_BF16) {
+      unpack_bf16x8(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(src) + at), x);
+    } else {
+      const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(src) + at);
+      const float4 a = f[0], b = f[1];
+      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    // magnitudes compare as integers, NaN above infinity
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
+    m = max(m, (uint32_t)__shfl_xor((int)m, 1, 64));
+    m = max(m, (uint32_t)__shfl_xor((int)m, 2, 64));
+    const int code = scale_code<FMT>(__uint_as_float(m));
+    // a group that reads as NaN stores zeros
+    const float sc = scale_of(code == kScaleNan ? kScaleBias : code);
+    if (code == kScaleNan) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+    }
+    if constexpr (FMT == DKV_CACHE_FP8) *reinterpret_cast<uint2 *>(dst + r * D + 8 * ch) = quantise_fp8(x, sc);
+    else *reinterpret_cast<uint32_t *>(dst + r * (D / 2) + 4 * ch) = quantise_fp4(x, sc);
+    if ((ch & 3) == 0) (z ? c.vs : c.ks)[r * (D / kGroup) + ch / 4] = (uint8_t)code;
+  }
+}
+
+// Thread = 8 elements of row i of bank (s, h), K or V.
+template <int DT, int FMT, int D>
+__global__ __launch_bounds__(kThreads) void k_cache_read(Pages c, const int32_t *__restrict__ first, int n, void *k, void *v,
+                                                         int nb) {
+  constexpr int CH = D / 8;
+  const int bz = (int)(blockIdx.x / (unsigned)nb), z = bz & 1, b = bz >> 1, s = b / c.H, h = b % c.H;
+  const int item = (int)(blockIdx.x % (unsigned)nb) * kThreads + (int)threadIdx.x;  // n CH <= 2^28
+  const int ch = item % CH, i = item / CH;
+  if (i >= n) return;
+  const int64_t pos = (int64_t)(first ? first[s] : 0) + i;
+  int p = -1;
+  if (pos >= 0 && pos < seq_length(c, s)) p = page_of(c, s, (int)pos);
+  const size_t r = p < 0 ? 0 : pool_row(c, p, h, (int)pos);
+  const unsigned char *src = z ? c.v : c.k;
+  const uint8_t *sc = z ? c.vs : c.ks;
+  const size_t o = (((size_t)b * n + i) * CH + ch) * 8;
+  if constexpr (DT == DKV_BF16) {
+    uint4 x = {0, 0, 0, 0};
+    if (p >= 0) x = load_bf16x8<FMT, D>(src, sc, r, ch);
+    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(z ? v : k) + o) = x;
+  } else {
+    float x[8] = {};
+    if (p >= 0) load_f32x8<DT, FMT, D>(src, sc, r, ch, x);
+    float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(z ? v : k) + o);
+    f[0] = float4{x[0], x[1], x[2], x[3]};
+    f[1] = float4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+template <int DT, int FMT, int D>
+hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, int64_t hs, hipStream_t s) {
+  const int most = c.max_new < c.T ? c.max_new : c.T;
+  constexpr int kRows = kThreads / (D / 8);
+  const int64_t nb = ((int64_t)most * c.H + kRows - 1) / kRows, grid = nb * c.S * 2;
+  if (grid == 0) return hipSuccess;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  k_cache_write<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);
+  return hipGetLastError();
+}
+template <int DT, int FMT, int D>
+hipError_t read_impl(const Pages &c, const int32_t *first, int n, void *k, void *v, hipStream_t s) {
+  const int64_t nb = ((int64_t)n * (D / 8) + kThreads - 1) / kThreads, grid = nb * c.S * c.H * 2;
+  if (grid == 0) return hipSuccess;
+  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  k_cache_read<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, first, n, k, v, (int)nb);
+  return hipGetLastError();
+}
+
+template <class F>
+hipError_t by_format(int dtype, int fmt, int d, F f) {
+#define DKV_CASE(DT, FMT, D) \
+  if (dtype == DT && fmt == FMT && d == D) return f(std::integral_constant<int, DT>(), std::integral_constant<int, FMT>(), \
+                                                    std::integral_constant<int, D>());
+  DKV_CASE(DKV_BF16, DKV_CACHE_FULL, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FULL, 128)
+  DKV_CASE(DKV_BF16, DKV_CACHE_FP8, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FP8, 128)
+  DKV_CASE(DKV_BF16, DKV_CACHE_FP4, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FP4, 128)
+  DKV_CASE(DKV_F32, DKV_CACHE_FULL, 64) DKV_CASE(DKV_F32, DKV_CACHE_FULL, 128)
+  DKV_CASE(DKV_F32, DKV_CACHE_FP8, 64) DKV_CASE(DKV_F32, DKV_CACHE_FP8, 128)
+  DKV_CASE(DKV_F32, DKV_CACHE_FP4, 64) DKV_CASE(DKV_F32, DKV_CACHE_FP4, 128)
+#undef DKV_CASE
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const void *k, const void *v, int64_t ts,
+                              int64_t hs, hipStream_t s) {
+  return by_format(dtype, fmt, d, [&](auto dt, auto f, auto dd) {
+    return write_impl<decltype(dt)::value, decltype(f)::value, decltype(dd)::value>(c, k, v, ts, hs, s);
+  });
+}
+
+hipError_t launch_cache_read(const Pages &c, int dtype, int fmt, int d, const int32_t *first, int n, void *k, void *v,
+                             hipStream_t s) {
+  return by_format(dtype, fmt, d, [&](auto dt, auto f, auto dd) {
+    return read_impl<decltype(dt)::value, decltype(f)::value, decltype(dd)::value>(c, first, n, k, v, s);
+  });
+}
+
+}  // namespace dkv

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/densitykv.h"
+#include "dkv_cache.hpp"
 
 namespace dkv {
 
@@ -114,6 +115,29 @@ struct KvSeg {
 hipError_t launch_attention(const dkv_bank &bank, const void *q, int nq, KvSeg win, KvSeg sink,
                             void *out, float scale, const Geom &g, void *ws, int nsplit, hipStream_t s);
 int attention_splits(const dkv_bank &bank, int nq, int nw, int ns, size_t *bytes);
+// The paged window cache (dkv_cache.hip, dkv_cache_attention.hip).
+hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const void *k, const void *v, int64_t token_stride,
+                              int64_t head_stride, hipStream_t s);
+hipError_t launch_cache_read(const Pages &c, int dtype, int fmt, int d, const int32_t *first, int n, void *k, void *v,
+                             hipStream_t s);
+// Queries and outputs of an attention call; bank: the live slots that every query sees as well (capacity 0: none).
+struct CacheQueries {
+  const void *q;
+  void *out;
+  int64_t qt, qh, ot, oh;  // strides in elements
+  int nh, G;               // query heads, and query heads per kv head
+  float scale_log2;        // softmax scale times log2(e)
+};
+struct BankRows {
+  const void *k, *v;
+  const int32_t *occupancy, *budget;
+  int cap;
+};
+hipError_t launch_cache_attention(const Pages &c, int dtype, int fmt, int d, const Mask &mask, const BankRows &bank,
+                                  const CacheQueries &qs, void *ws, int nsplit, hipStream_t s);
+// Splits the launch takes (1: none) and the bytes of its partial results.
+int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask &mask, const BankRows &bank, int nh,
+                           size_t *bytes);
 // Stages: the score (exact, or approximate with the order made exact afterwards: kGramOrder for the positions the
 // first part of the crossing search reads, kGramOrderRest for the others of open groups), the crossing search in
 // two parts, the projected densities, the maintenance.
