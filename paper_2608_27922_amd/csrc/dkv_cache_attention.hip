@@ -1,7 +1,9 @@
 // Attention of new tokens over [bank; paged window cache] on gfx950.
 //
 // out = softmax(q K^T * scale) V over the tokens that a query sees (dkv_cache.hpp:
-// seen_by) and the live slots of its bank.
+// seen_by) and the live slots of its bank.  The rows of one (sequence, kv head) are
+// its (token, query head) pairs, tokens first; a row block of them walks key tiles in
+// the order bank, first tokens, window with a streaming softmax in fp32.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -11,113 +13,1111 @@
 namespace dkv {
 namespace {
 
-// One wave per (token, head): scores of 64 keys at a time, one key per lane, an online
-// softmax, then the weighted values with 8 columns per lane.
-template <int DT, int FMT, int D>
-__global__ __launch_bounds__(64) void k_cache_attn_row(Pages c, Mask mask, BankRows bank, CacheQueries qs) {
-  constexpr int CH = D / 8, KG = 64 / CH;
-  const unsigned nrow = (unsigned)c.max_new * qs.nh;
-  const int s = (int)(blockIdx.x / nrow), row = (int)(blockIdx.x % nrow), i = row / qs.nh, hq = row % qs.nh;
-  const NewRows nr = new_rows(c, s);
-  if (i >= nr.n) return;
-  const int l = threadIdx.x, h = hq / qs.G, b = s * c.H + h;
-  const int len = seq_length(c, s);
-  const Seen seen = seen_by(mask, len, nr.n, i);
-  __shared__ float ql[D];
-  __shared__ float pl[64];
-  const size_t t = (size_t)nr.first + i;
-  for (int j = l; j < D; j += 64) ql[j] = load_elem<DT>(qs.q, t * qs.qt + (size_t)hq * qs.qh + j);
-  __syncthreads();
-  float mx = -INFINITY, sum = 0.0f, o[8] = {};
-  bool any = false;
-  auto tile = [&](int n, auto valid, auto load_k, auto load_v) {
-    for (int j0 = 0; j0 < n; j0 += 64) {
-      const int j = j0 + l;
-      const bool ok = j < n && valid(j);
-      if (!__any(ok)) continue;
-      any = true;
-      float sc = -INFINITY;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int kBufferRsrcWord3 = 0x00020000;  // raw buffer, 32-bit data, no swizzle
+constexpr float kLazyLimit = 65536.0f;        // weights of a tile's row under the running reference, see exps()
+
+// Partial results of split keys: for split s and row (s * max_new + i) * nh + head, the
+// running maximum (bf16: raw scores) and weight sum, and the unnormalised output.
+struct Part {
+  float *o;    // [nsplit, rows, D]
+  float2 *ml;  // [nsplit, rows]; null without splits
+};
+
+// Key tiles (KT keys each) of the rows of tokens i0..i1: nb bank tiles, a1 tiles of the
+// first tokens, then the window's tiles from b0.  hi, lo: positions that any row sees.
+struct Plan {
+  int nb, a1, b0, total, hi, lo, m;
+};
+template <int KT>
+__device__ __forceinline__ Plan plan_of(const Mask &mask, const BankRows &bank, int b, int len, int n, int i0, int i1) {
+  Plan p;
+  p.m = bank.cap > 0 ? bound(bank.occupancy[b], 0, bound(bank.budget[b], 0, bank.cap)) : 0;
+  p.hi = seen_by(mask, len, n, i1).hi;
+  p.lo = min(seen_by(mask, len, n, i0).lo, p.hi);
+  p.nb = (p.m + KT - 1) / KT;
+  p.a1 = p.lo > 0 ? (min(mask.sink, p.hi) + KT - 1) / KT : 0;
+  p.b0 = max(p.lo / KT, p.a1);
+  p.total = p.nb + p.a1 + max(0, (p.hi + KT - 1) / KT - p.b0);
+  return p;
+}
+__device__ __forceinline__ int tile_pos(const Plan &p, int KT, int t) {
+  const int u = t - p.nb;
+  return KT * (u < p.a1 ? u : u - p.a1 + p.b0);
+}
+
+// The host sizes the splits by the largest sequence; of them a row block takes as many as
+// leave each at least LEAST tiles (one at least), in equal runs.
+template <int LEAST>
+__device__ __forceinline__ int splits_used(int total, int nsplit) {
+  return max(1, min(nsplit, total / LEAST));
+}
+__device__ __forceinline__ void split_range(int total, int used, int split, int &t0, int &t1) {
+  const int per = (total + used - 1) / used;
+  t0 = min(total, split * per);
+  t1 = min(total, t0 + per);
+}
+
+// Page numbers of 128 consecutive columns of a sequence's table, 64 in each of two
+// registers of a wave (one per lane), the second on its way while the first is used.
+struct PageWindow {
+  const int32_t *row;
+  int cols, P, base, cur, nxt;
+  __device__ __forceinline__ int load(int c0) const {
+    const int col = c0 + (int)(threadIdx.x & 63);
+    const int p = col < cols ? row[col] : -1;
+    return (unsigned)p < (unsigned)P ? p : -1;
+  }
+  __device__ __forceinline__ void init(const Pages &c, int s) {
+    row = c.table + (size_t)s * c.cols;
+    cols = c.cols;
+    P = c.P;
+    base = -256;
+  }
+  // columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page)
+  __device__ __forceinline__ void seek(int col) {
+    if (col >= base && col < base + 64) return;
+    if (col >= base + 64 && col < base + 128) {
+      cur = nxt;
+      base += 64;
+    } else {
+      base = col & ~63;
+      cur = load(base);
+    }
+    nxt = load(base + 64);
+  }
+  __device__ __forceinline__ int page(int col) const { return __builtin_amdgcn_readlane(cur, col - base); }
+};
+
+// Physical 16-byte chunk of logical chunk c of row r (K: conflict-free 16-byte reads of
+// one chunk across 16 rows; V: conflict-free transposed 8-byte reads of 4 chunks across
+// 4 rows).
+template <int D>
+__device__ __forceinline__ int k_swz(int r, int c) { return c ^ (r % (D / 8)); }
+template <int D>
+__device__ __forceinline__ int v_swz(int r, int c) { return c ^ ((4 * (r % 4)) % (D / 8)); }
+
+// Direct-to-LDS loads of 8 rows (2 D bytes each, `valid` of them, the others as zeros)
+// of K and V into rows r0 .. r0 + 7 of a tile.  Lane i of a 1 KB load fetches the
+// logical chunk that belongs at 16 i.
+template <int D>
+struct Rows8 {
+  static constexpr int kLoads = 16 * D / 1024;  // per tensor
+  int rsub, pc, v[kLoads];                      // row and physical chunk of this lane in a load; V's byte offsets
+};
+template <int D>
+__device__ __forceinline__ Rows8<D> rows8_offsets() {
+  constexpr int CH = D / 8, RPL = 64 / CH;
+  const int l = threadIdx.x & 63;
+  Rows8<D> o;
+  o.rsub = l / CH;
+  o.pc = l % CH;
+#pragma unroll
+  for (int q = 0; q < Rows8<D>::kLoads; ++q) {
+    const int r = q * RPL + o.rsub;
+    o.v[q] = r * (2 * D) + 16 * v_swz<D>(r, o.pc);
+  }
+  return o;
+}
+// K's swizzle depends on the row modulo D / 8, V's modulo 4.
+template <int D>
+__device__ __forceinline__ void rows8_issue(int rsub, int pc, const int *voff, const unsigned char *kp,
+                                            const unsigned char *vp, int valid, int r0, char *kt, char *vt) {
+  constexpr int RPL = 512 / D;
+  const __amdgpu_buffer_rsrc_t rk =
+      __builtin_amdgcn_make_buffer_rsrc((void *)kp, (short)0, valid * (2 * D), kBufferRsrcWord3);
+  const __amdgpu_buffer_rsrc_t rv =
+      __builtin_amdgcn_make_buffer_rsrc((void *)vp, (short)0, valid * (2 * D), kBufferRsrcWord3);
+#pragma unroll
+  for (int q = 0; q < Rows8<D>::kLoads; ++q) {
+    const int r = q * RPL + rsub, koff = r * (2 * D) + 16 * k_swz<D>(r0 + r, pc);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void *)(kt + r0 * (2 * D) + q * 1024), 16, koff, 0, 0, 0);
+  }
+#pragma unroll
+  for (int q = 0; q < Rows8<D>::kLoads; ++q)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void *)(vt + r0 * (2 * D) + q * 1024), 16, voff[q], 0, 0, 0);
+}
+
+// A quarter row (D / 4 elements) on its way from memory to an LDS tile through registers.
+template <int FMT, int D>
+struct Quarter {
+  u32x4 x[D / 32];  // bank rows take all of it, FP8 rows half, FP4 rows a quarter
+  int code;
+  __device__ __forceinline__ void load_bank(const uint16_t *row, int part, bool ok) {
+#pragma unroll
+    for (int e = 0; e < D / 32; ++e) {
+      x[e] = u32x4{0, 0, 0, 0};
+      if (ok) x[e] = *reinterpret_cast<const u32x4 *>(row + part * (D / 4) + 8 * e);
+    }
+  }
+  __device__ __forceinline__ void load(const unsigned char *pool, const uint8_t *scale, size_t row, int part, bool ok) {
+    code = kScaleBias;
+    x[0] = u32x4{0, 0, 0, 0};
+    if constexpr (FMT == DKV_CACHE_FP8) {
+      if constexpr (D == 128) x[1] = u32x4{0, 0, 0, 0};
       if (ok) {
-        float dot = 0.0f, x[8];
-        for (int ch = 0; ch < CH; ++ch) {
-          load_k(j, ch, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dot = __builtin_fmaf(x[e], ql[8 * ch + e], dot);
-        }
-        sc = dot * qs.scale_log2;
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(pool + row * D + part * (D / 4));
+        x[0] = p[0];
+        if constexpr (D == 128) x[1] = p[1];
       }
-      float tm = sc;
-      for (int w = 32; w; w >>= 1) tm = fmaxf(tm, __shfl_xor(tm, w, 64));
-      const float mn = fmaxf(mx, tm), ref = mn == -INFINITY ? 0.0f : mn;
-      const float corr = exp2f(mx - ref);
-      mx = mn;
-      const float p = ok ? exp2f(sc - ref) : 0.0f;
-      __syncthreads();
-      pl[l] = ok ? p : -1.0f;
-      __syncthreads();
-      float ps = p;
-      for (int w = 32; w; w >>= 1) ps += __shfl_xor(ps, w, 64);
-      sum = sum * corr + ps;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] *= corr;
-      for (int g = l / CH; g < 64; g += KG) {
-        const float pg = pl[g];
-        if (pg == -1.0f) continue;
-        float x[8];
-        load_v(j0 + g, l % CH, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(pg, x[e], o[e]);
+    } else {
+      if (ok) {
+        const unsigned char *p = pool + row * (D / 2) + part * (D / 8);
+        if constexpr (D == 128) {
+          x[0] = *reinterpret_cast<const u32x4 *>(p);
+        } else {
+          const u32x2 y = *reinterpret_cast<const u32x2 *>(p);
+          x[0] = u32x4{y[0], y[1], 0, 0};
+        }
       }
     }
-  };
-  if (bank.cap > 0) {
-    const int m = bound(bank.occupancy[b], 0, bound(bank.budget[b], 0, bank.cap));
-    const size_t r0 = (size_t)b * bank.cap;
-    tile(m, [](int) { return true; },
-         [&](int j, int ch, float *x) { load_f32x8<DT, DKV_CACHE_FULL, D>((const unsigned char *)bank.k, nullptr, r0 + j, ch, x); },
-         [&](int j, int ch, float *x) { load_f32x8<DT, DKV_CACHE_FULL, D>((const unsigned char *)bank.v, nullptr, r0 + j, ch, x); });
+    if (ok) code = scale[row * (D / kGroup) + part * (D / 4) / kGroup];
   }
-  tile(seen.hi, [&](int j) { return sees(seen, mask.sink, j) && page_of(c, s, j) >= 0; },
-       [&](int j, int ch, float *x) { load_f32x8<DT, FMT, D>(c.k, c.ks, pool_row(c, page_of(c, s, j), h, j), ch, x); },
-       [&](int j, int ch, float *x) { load_f32x8<DT, FMT, D>(c.v, c.vs, pool_row(c, page_of(c, s, j), h, j), ch, x); });
-  for (int w = CH; w < 64; w <<= 1)
+  template <bool V>
+  __device__ __forceinline__ void store(char *tile, int r, int part, bool bank) const {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] += __shfl_xor(o[e], w, 64);
-  if (l >= CH) return;
-  // nothing seen: zeros; scores of -inf alone: NaN
-  const float inv = sum > 0.0f ? 1.0f / sum : (any ? NAN : 0.0f);
-  const size_t at = t * qs.ot + (size_t)hq * qs.oh + 8 * l;
-  if constexpr (DT == DKV_BF16)
-    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(qs.out) + at) =
-        uint4{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv), pack_bf16x2(o[4] * inv, o[5] * inv),
-              pack_bf16x2(o[6] * inv, o[7] * inv)};
-  else {
-    float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(qs.out) + at);
-    f[0] = float4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-    f[1] = float4{o[4] * inv, o[5] * inv, o[6] * inv, o[7] * inv};
+    for (int e = 0; e < D / 32; ++e) {
+      uint4 y;
+      if (bank) y = uint4{x[e][0], x[e][1], x[e][2], x[e][3]};
+      else if constexpr (FMT == DKV_CACHE_FP8) y = bf16_of_fp8(uint2{x[e / 2][2 * (e & 1)], x[e / 2][2 * (e & 1) + 1]}, code);
+      else y = bf16_of_fp4(x[0][e], code);
+      const int ch = part * (D / 32) + e;
+      *reinterpret_cast<uint4 *>(tile + r * (2 * D) + 16 * (V ? v_swz<D>(r, ch) : k_swz<D>(r, ch))) = y;
+    }
+  }
+};
+
+// s_waitcnt immediate: at most n vector-memory operations and no LDS operation outstanding.
+constexpr int waitcnt_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
+__device__ __forceinline__ void stage_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// What one wave (32 rows, row n = lane % 32, half h = lane / 32) keeps while it walks keys.
+template <int D>
+struct Rows {
+  f32x16 o[D / 32];  // O^T: register i of tile t is element 32 t + 8 (i / 4) + 4 h + i % 4
+  float mrun, lrun;
+  bool any;          // this lane saw a key of its row
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
+    mrun = -INFINITY, lrun = 0.0f, any = false;
+  }
+};
+
+// 1 for +inf, 128 for -inf, 16384 for NaN, 0 for finite values, as bf16: sums of 64 of them
+// are exact in fp32.
+__device__ __forceinline__ uint32_t kind_of(uint32_t half) {
+  const uint32_t a = half & 0x7fffu;
+  return a < 0x7f80u ? 0u : (a > 0x7f80u ? 0x4680u : ((half & 0x8000u) ? 0x4300u : 0x3f80u));
+}
+__device__ __forceinline__ float value_of_kinds(float c) {
+  if (c == 0.0f) return 0.0f;
+  const bool nan = c >= 16384.0f;
+  const int r = (int)c & 16383;
+  const bool neg = r >= 128, pos = (r & 127) != 0;
+  return nan || (pos && neg) ? NAN : (neg ? -INFINITY : INFINITY);
+}
+
+// S^T = K Q^T for NSUB x 32 keys of an LDS tile.
+template <int D, int NSUB>
+__device__ __forceinline__ void scores(const char *kt, const bf16x8 *qf, f32x16 *sc) {
+  const int l = threadIdx.x & 63, h = l >> 5, n = l & 31;
+#pragma unroll
+  for (int sub = 0; sub < NSUB; ++sub) {
+    const int key = 32 * sub + n;
+    bf16x8 a[D / 16];
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk)
+      a[kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(kt + key * (2 * D) + 16 * k_swz<D>(key, 2 * kk + h)));
+    f32x16 acc = {};
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk], qf[kk], acc, 0, 0, 0);
+    sc[sub] = acc;
+  }
+}
+
+// A operand of 16 keys (K step kst of sub-tile sub) of V^T, columns 32 t2 ..: the transposing
+// LDS reads give lane groups of 16 their 4 x 16 blocks; the key order inside the step is
+// that of the weights' registers.
+template <int D>
+__device__ __forceinline__ u32x4 v_operand(const char *vt, int sub, int kst, int t2) {
+  const int l = threadIdx.x & 63, gq = l >> 4, cq = l & 15;
+  const int ka = 32 * sub + 16 * kst + 4 * (gq >> 1) + (cq >> 2), kb = ka + 8;
+  const int dvb = 8 * t2 + 4 * (gq & 1) + (cq & 3);
+  const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_i16x4 *)(vt + ka * (2 * D) + 16 * v_swz<D>(ka, dvb >> 1) + 8 * (dvb & 1)));
+  const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_i16x4 *)(vt + kb * (2 * D) + 16 * v_swz<D>(kb, dvb >> 1) + 8 * (dvb & 1)));
+  const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+  return u32x4{a[0], a[1], b[0], b[1]};
+}
+
+// Whether this lane or the row's other lane says so (every lane takes part in the exchange).
+__device__ __forceinline__ bool either_half(bool x) {
+  const int y = __shfl_xor((int)x, 32, 64);
+  return x | (y != 0);
+}
+
+// Softmax update of one tile of one wave from its scores (masked ones are -inf); pb: the
+// weights in bf16, pairs of registers.  The reference maximum is raised only when a lane's
+// sum of weights exceeds 2^16 (or is not finite): weights and sums stay far from overflow,
+// and the final division removes the common factor.
+template <int D, int NSUB>
+__device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t (*pb)[8], float c) {
+  const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+  float psum = 0.0f;
+  auto exps = [&](float moff) {
+    psum = 0.0f;
+#pragma unroll
+    for (int sub = 0; sub < NSUB; ++sub) {
+      float ps = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i], c, moff));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i + 1], c, moff));
+        pb[sub][i >> 1] = pack_bf16x2(p0, p1);
+        // row sum of the bf16 weights that are multiplied into O: their rounding (2^-8) enters
+        // numerator and denominator alike
+        ps = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[sub][i >> 1]), ones, ps, false);
+      }
+      psum += ps;
+    }
+  };
+  exps(-r.mrun * c);
+  const bool over = !(psum <= kLazyLimit);
+  if (__any(over)) {
+    // only the rows concerned, so that a row's result does not depend on the rows beside it
+    const bool raise = either_half(over);
+    float tmax = sc[0][0];
+#pragma unroll
+    for (int sub = 0; sub < NSUB; ++sub)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) tmax = fmaxf(tmax, sc[sub][i]);
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+    const float mnew = raise ? fmaxf(r.mrun, tmax) : r.mrun;
+    const float mref = mnew == -INFINITY ? 0.0f : mnew;  // scores of -inf alone: weights 0, not inf - inf
+    const float corr = raise ? __builtin_amdgcn_exp2f((r.mrun - mref) * c) : 1.0f;
+    r.mrun = mnew;
+    r.lrun *= corr;
+#pragma unroll
+    for (int t2 = 0; t2 < D / 32; ++t2)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r.o[t2][i] *= corr;
+    exps(-mref * c);
+  }
+  r.lrun += psum;
+}
+
+// O^T += V^T P^T.
+template <int D, int NSUB>
+__device__ __forceinline__ void product(Rows<D> &r, const uint32_t (*pb)[8], const char *vt) {
+#pragma unroll
+  for (int sub = 0; sub < NSUB; ++sub) {
+#pragma unroll
+    for (int kst = 0; kst < 2; ++kst) {
+      const u32x4 bp = {pb[sub][4 * kst], pb[sub][4 * kst + 1], pb[sub][4 * kst + 2], pb[sub][4 * kst + 3]};
+#pragma unroll
+      for (int t2 = 0; t2 < D / 32; ++t2)
+        r.o[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand<D>(vt, sub, kst, t2)),
+                                                          __builtin_bit_cast(bf16x8, bp), r.o[t2], 0, 0, 0);
+    }
+  }
+}
+
+// In a tile that some rows see in part, a NaN or an infinity of V would reach the others
+// through 0 x inf.  Such values are added to the rows that see them (vis: bit k of a lane
+// for key k + 4 h of its row), as sums of the kinds that a row sees, and become zeros in
+// the tile.  NT threads share the tile (all of them call this), one wave or a workgroup.
+template <int D, int NSUB, int NT>
+__device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool work) {
+  constexpr int kBytes = NSUB * 32 * 2 * D;
+  const int l = threadIdx.x & 63;
+  uint32_t bad = 0;
+#pragma unroll 4
+  for (int j = 0; j < kBytes / 1024; ++j) {
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(vt + j * 1024 + 16 * l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)  // an exponent of all ones plus one carries into its half's sign bit
+      bad |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  }
+  if (!__any(bad != 0)) return;
+  if (work) {
+#pragma unroll 1
+    for (int t2 = 0; t2 < D / 32; ++t2) {
+      f32x16 kinds = {};
+#pragma unroll 1
+      for (int st = 0; st < 2 * NSUB; ++st) {
+        u32x4 a = v_operand<D>(vt, st >> 1, st & 1, t2), bv;
+        const uint32_t w = (uint32_t)(vis >> (16 * st));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          a[e] = kind_of(a[e] & 0xffffu) | (kind_of(a[e] >> 16) << 16);
+          const int k = 8 * (e >> 1) + 2 * (e & 1);  // registers 2 e and 2 e + 1 of the step
+          bv[e] = ((w >> k) & 1 ? 0x3f80u : 0u) | ((w >> (k + 1)) & 1 ? 0x3f800000u : 0u);
+        }
+        kinds = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, bv), kinds,
+                                                        0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float x = value_of_kinds(kinds[i]);
+#pragma unroll
+        for (int u = 0; u < D / 32; ++u)
+          if (u == t2) r.o[u][i] += x;
+      }
+    }
+  }
+  if constexpr (NT > 64) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    stage_barrier();  // every wave has read the tile
+  }
+  for (int j = (NT > 64 ? (int)threadIdx.x : l); j < kBytes / 16; j += NT) {
+    u32x4 x = *reinterpret_cast<const u32x4 *>(vt + 16 * j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+      if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+    }
+    *reinterpret_cast<u32x4 *>(vt + 16 * j) = x;
+  }
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  if constexpr (NT > 64) stage_barrier();
+}
+
+// Which of the wave's rows see which keys of a tile.
+struct WaveMask {
+  Seen first, last, row;  // of the wave's first and last row, and of this lane's
+  int sink;
+  __device__ __forceinline__ bool none(int pos, int KT) const {
+    return pos >= last.hi || (pos + KT <= first.lo && pos >= sink);
+  }
+  __device__ __forceinline__ bool all(int pos, int KT) const {
+    return pos + KT <= first.hi && (pos >= last.lo || pos + KT <= sink);
+  }
+};
+
+// Bits below x of 64.
+__device__ __forceinline__ uint64_t bits_below(int x) { return x <= 0 ? 0 : (x >= 64 ? ~0ull : (1ull << x) - 1); }
+
+// Keys of the tile at pos that this lane's row sees, bit k for key k + 4 h (so that the bits
+// of the lane's score registers are at 8 (i / 4) + i % 4); present: the tile's keys in pages
+// that are there.
+__device__ __forceinline__ uint64_t visible_bits(const WaveMask &w, int pos, uint64_t present) {
+  const uint64_t m = bits_below(w.row.hi - pos) & (~bits_below(w.row.lo - pos) | bits_below(w.sink - pos)) & present;
+  return m >> (4 * ((threadIdx.x & 63) >> 5));
+}
+template <int NSUB>
+__device__ __forceinline__ bool mask_cache(f32x16 *sc, uint64_t vis) {
+  constexpr uint64_t mine = NSUB == 2 ? 0x0f0f0f0f0f0f0f0full : 0x0f0f0f0full;
+#pragma unroll
+  for (int sub = 0; sub < NSUB; ++sub)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!((uint32_t)(vis >> (32 * sub)) & (1u << (8 * (i >> 2) + (i & 3))))) sc[sub][i] = -INFINITY;
+  return (vis & mine) != 0;
+}
+template <int NSUB>
+__device__ __forceinline__ void mask_bank(f32x16 *sc, int nvalid) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int sub = 0; sub < NSUB; ++sub)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (32 * sub + 8 * (i >> 2) + 4 * h + (i & 3) >= nvalid) sc[sub][i] = -INFINITY;
+}
+
+// Bits of the keys of the tile of KT tokens at pos that lie in pages that are there.
+template <int KT>
+__device__ __forceinline__ uint64_t present_keys(const PageWindow &pw, int pos, int lps) {
+  const int c0 = pos >> lps;
+  if ((1 << lps) >= KT) return pw.page(c0) >= 0 ? ~0ull : 0ull;
+  uint64_t bits = 0;
+  for (int j = 0; j < KT >> lps; ++j)
+    if (pw.page(c0 + j) >= 0) bits |= ((1ull << (1 << lps)) - 1) << (j << lps);
+  return KT == 64 ? bits : (bits | ~0xffffffffull);
+}
+
+// Weight sum of a row: NaN-marked (-1) where its keys' scores were all -inf.
+__device__ __forceinline__ float row_sum(float mx, float l, bool keys) {
+  return keys && mx == -INFINITY && l == 0.0f ? -1.0f : l;
+}
+__device__ __forceinline__ float inv_sum(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : NAN); }
+
+// Row r (token, head of the group) of a row block -> its packed row and query head.
+struct RowAt {
+  size_t t;
+  int i, hq;
+};
+__device__ __forceinline__ RowAt row_at(const NewRows &nr, const CacheQueries &qs, int h, int r) {
+  const int i = (int)((unsigned)r / (unsigned)qs.G);
+  return RowAt{(size_t)(nr.first + i), i, h * qs.G + (r - i * qs.G)};
+}
+
+template <int D>
+__device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const RowAt &a, bool ok) {
+  const int h = (threadIdx.x & 63) >> 5;
+  const uint16_t *q = static_cast<const uint16_t *>(qs.q) + a.t * qs.qt + (size_t)a.hq * qs.qh;
+#pragma unroll
+  for (int kk = 0; kk < D / 16; ++kk) {
+    u32x4 x = {0, 0, 0, 0};
+    if (ok) x = *reinterpret_cast<const u32x4 *>(q + 16 * kk + 8 * h);
+    qf[kk] = __builtin_bit_cast(bf16x8, x);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows (bf16): a workgroup of 8 waves owns 256 rows, 32 per wave, and walks tiles of
+// 64 keys that its waves load together.
+// ---------------------------------------------------------------------------
+constexpr int kWWaves = 8, kWRows = 32 * kWWaves, kWK = 64, kWLeast = 4;
+
+template <int FMT, int D>
+__global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Mask mask, BankRows bank, CacheQueries qs,
+                                                                    int nrb, int nsplit, Part part) {
+  constexpr int TB = kWK * 2 * D;
+  constexpr bool FULL = FMT == DKV_CACHE_FULL;
+  // Workgroup L runs on XCD L % 8: rank the workgroups XCD by XCD, so that the row blocks that
+  // read the same keys share an L2; the later row blocks (longest under a causal mask) first.
+  const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
+  const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
+  const int rb = nrb - 1 - p % nrb, bs = p / nrb, b = bs / nsplit, split = bs % nsplit;
+  const int s = b / c.H, h = b % c.H;
+  const NewRows nr = new_rows(c, s);
+  const int nrows = min(nr.n, c.max_new) * qs.G, r0 = rb * kWRows;
+  if (r0 >= nrows) return;
+  const int len = seq_length(c, s);
+  const int r1 = min(r0 + kWRows, nrows) - 1;
+  const Plan pl = plan_of<kWK>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G);
+  const int used = splits_used<kWLeast>(pl.total, nsplit);
+  if (split >= used) return;
+  int tb, nt;
+  split_range(pl.total, used, split, tb, nt);
+
+  __shared__ __attribute__((aligned(1024))) char k0[TB], k1[TB], k2[FULL ? TB : 16];
+  __shared__ __attribute__((aligned(1024))) char v0[TB], v1[TB], v2[FULL ? TB : 16];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
+  const int w0 = r0 + 32 * wave;
+  const bool work = w0 < nrows;  // a wave past the last row only loads
+  const int r = min(w0 + n, nrows - 1);
+  const RowAt at = row_at(nr, qs, h, r);
+  const bool rv = w0 + n < nrows;
+  bf16x8 qf[D / 16];
+  load_q<D>(qf, qs, at, rv);
+  Rows<D> rows;
+  rows.init();
+  WaveMask wm;
+  wm.sink = mask.sink;
+  wm.row = seen_by(mask, len, nr.n, at.i);
+  wm.first = seen_by(mask, len, nr.n, min(w0, nrows - 1) / qs.G);
+  wm.last = seen_by(mask, len, nr.n, min(w0 + 31, nrows - 1) / qs.G);
+  PageWindow pw;   // of the tile being loaded
+  pw.init(c, s);
+
+  const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (2 * D);
+  const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (2 * D);
+
+  const Seen bfirst = seen_by(mask, len, nr.n, r0 / qs.G), blast = seen_by(mask, len, nr.n, r1 / qs.G);
+  auto compute = [&](int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
+    const bool isbank = t < pl.nb;
+    const int pos = tile_pos(pl, kWK, t);
+    const bool act = work && (isbank || !wm.none(pos, kWK));
+    // whether every row of the workgroup sees all of the tile: the same for all its waves
+    const bool whole = isbank || (present == ~0ull && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
+    uint32_t pb[2][8];
+    uint64_t vis = 0;
+    if (act) {
+      f32x16 sc[2];
+      scores<D, 2>(kt, qf, sc);
+      if (isbank) {
+        const int nv = pl.m - t * kWK;
+        if (nv < kWK) mask_bank<2>(sc, nv);
+        rows.any = true;
+      } else if (whole) {
+        rows.any = true;
+      } else {
+        vis = visible_bits(wm, pos, present);
+        rows.any |= mask_cache<2>(sc, vis);
+      }
+      softmax_update<D, 2>(rows, sc, pb, qs.scale_log2);
+    }
+    if (!whole) purge<D, 2, 64 * kWWaves>(rows, vt, vis, act);
+    if (act) product<D, 2>(rows, pb, vt);
+  };
+
+  if constexpr (FULL) {
+    // K and V tiles go global -> LDS without registers, three stages: two tiles in flight
+    // while one is used.  A wave loads 8 rows of each tile, which lie in one page.
+    const Rows8<D> ld = rows8_offsets<D>();
+    uint64_t pr[3] = {0, 0, 0};
+    auto issue = [&](int t, char *kd, char *vd) -> uint64_t {
+      if (t >= nt) return 0;
+      if (t < pl.nb) {
+        const int r8 = t * kWK + 8 * wave;
+        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8), 8 * wave, kd, vd);
+        return ~0ull;
+      }
+      const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
+      pw.seek(pos >> c.lps);
+      const int page = pw.page(p8 >> c.lps);
+      int nv = bound(pl.hi - p8, 0, 8);
+      if (page < 0 || (p8 + 8 <= pl.lo && p8 >= mask.sink)) nv = 0;
+      const size_t row = pool_row(c, page < 0 ? 0 : page, h, p8);
+      rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * wave, kd, vd);
+      return present_keys<kWK>(pw, pos, c.lps);
+    };
+    constexpr int kTileLoads = 2 * Rows8<D>::kLoads;
+    auto step = [&](int t, const char *kt, char *vt, uint64_t present, char *kn, char *vn) __attribute__((always_inline)) {
+      if (t + 1 < nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
+      else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      stage_barrier();
+      const uint64_t nx = issue(t + 2, kn, vn);
+      compute(t, kt, vt, present);
+      return nx;
+    };
+    pr[0] = issue(tb, k0, v0);
+    pr[1] = issue(tb + 1, k1, v1);
+    for (int t = tb; t < nt; t += 3) {
+      pr[2] = step(t, k0, v0, pr[0], k2, v2);
+      if (t + 1 < nt) pr[0] = step(t + 1, k1, v1, pr[1], k0, v0);
+      if (t + 2 < nt) pr[1] = step(t + 2, k2, v2, pr[2], k1, v1);
+    }
+  } else {
+    // Quantised rows come through registers and are stored as bf16: waves 0-3 a quarter row
+    // of K per lane, waves 4-7 of V, each wave 16 rows that lie in one page.
+    const bool isv = wave >= 4;
+    const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
+    Quarter<FMT, D> x;
+    uint64_t pcur = 0, pnext = 0;
+    bool bnext = false;
+    auto fetch = [&](int t) {
+      if (t >= nt) return;
+      bnext = t < pl.nb;
+      if (bnext) {
+        const int slot = t * kWK + lr;
+        x.load_bank(reinterpret_cast<const uint16_t *>(isv ? bv : bk) + (size_t)slot * D, qpart, slot < pl.m);
+        pnext = ~0ull;
+        return;
+      }
+      const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
+      pw.seek(pos >> c.lps);
+      const int page = pw.page(p16 >> c.lps);
+      const bool ok = page >= 0 && pos + lr < pl.hi && (p16 + 16 > pl.lo || p16 < mask.sink);
+      const size_t row = pool_row(c, page < 0 ? 0 : page, h, pos + lr);
+      x.load(isv ? c.v : c.k, isv ? c.vs : c.ks, row, qpart, ok);
+      pnext = present_keys<kWK>(pw, pos, c.lps);
+    };
+    auto put = [&](char *kd, char *vd) {
+      if (isv) x.template store<true>(vd, lr, qpart, bnext);
+      else x.template store<false>(kd, lr, qpart, bnext);
+    };
+    auto step = [&](int t, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
+      const uint64_t present = pcur;
+      if (t + 1 < nt) {
+        put(kn, vn);
+        pcur = pnext;
+        fetch(t + 2);
+      }
+      compute(t, kt, vt, present);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
+      stage_barrier();
+    };
+    if (tb < nt) {
+      fetch(tb);
+      put(k0, v0);
+      pcur = pnext;
+      fetch(tb + 1);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      stage_barrier();
+    }
+    for (int t = tb; t < nt; t += 2) {
+      step(t, k0, v0, k1, v1);
+      if (t + 1 < nt) step(t + 1, k1, v1, k0, v0);
+    }
+  }
+  if (!work) return;
+  const bool any = either_half(rows.any);
+  const float ltot = row_sum(rows.mrun, rows.lrun + __shfl_xor(rows.lrun, 32, 64), any);
+  if (!rv) return;
+  if (part.ml) {
+    const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
+    const size_t row = (size_t)split * nrow + ((size_t)s * c.max_new + at.i) * qs.nh + at.hq;
+    if (lh == 0) part.ml[row] = float2{rows.mrun, ltot};
+#pragma unroll
+    for (int t2 = 0; t2 < D / 32; ++t2)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4 *>(part.o + row * D + 32 * t2 + 8 * g + 4 * lh) =
+            float4{rows.o[t2][4 * g], rows.o[t2][4 * g + 1], rows.o[t2][4 * g + 2], rows.o[t2][4 * g + 3]};
+    return;
+  }
+  const float inv = inv_sum(ltot);
+  uint16_t *out = static_cast<uint16_t *>(qs.out) + at.t * qs.ot + (size_t)at.hq * qs.oh;
+#pragma unroll
+  for (int t2 = 0; t2 < D / 32; ++t2)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *reinterpret_cast<u32x2 *>(out + 32 * t2 + 8 * g + 4 * lh) =
+          u32x2{pack_bf16x2(rows.o[t2][4 * g] * inv, rows.o[t2][4 * g + 1] * inv),
+                pack_bf16x2(rows.o[t2][4 * g + 2] * inv, rows.o[t2][4 * g + 3] * inv)};
+}
+
+// ---------------------------------------------------------------------------
+// Few rows, and fp32: a workgroup of 4 waves owns 32 rows; each wave walks tiles of 32 keys of
+// its own (every fourth), and the four results are joined at the end.
+// ---------------------------------------------------------------------------
+constexpr int kFWaves = 4, kFK = 32, kFLeast = 4;
+
+// fp32 scores and products on v_mfma_f32_32x32x2_f32, keys and values straight from memory.
+// K step 4 c + j takes dims 8 c + j and 8 c + 4 + j of both operands.
+template <int FMT, int D>
+__device__ __forceinline__ float4 load_f32x4(const unsigned char *pool, const uint8_t *scale, size_t row, int d0) {
+  if constexpr (FMT == DKV_CACHE_FULL) {
+    return *reinterpret_cast<const float4 *>(pool + row * (4 * D) + 4 * d0);
+  } else {
+    const int code = scale[row * (D / kGroup) + d0 / kGroup];
+    uint32_t lo, hi;
+    if constexpr (FMT == DKV_CACHE_FP8) {
+      const uint4 y = bf16_of_fp8(uint2{*reinterpret_cast<const uint32_t *>(pool + row * D + d0), 0}, code);
+      lo = y.x, hi = y.y;
+    } else {
+      const uint4 y = bf16_of_fp4(*reinterpret_cast<const uint16_t *>(pool + row * (D / 2) + d0 / 2), code);
+      lo = y.x, hi = y.y;
+    }
+    return float4{__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16),
+                  __uint_as_float(hi & 0xffff0000u)};
+  }
+}
+template <int FMT, int D>
+__device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8_t *scale, size_t row, int d) {
+  if constexpr (FMT == DKV_CACHE_FULL) {
+    return *reinterpret_cast<const float *>(pool + row * (4 * D) + 4 * d);
+  } else {
+    const int code = scale[row * (D / kGroup) + d / kGroup];
+    uint32_t x;
+    if constexpr (FMT == DKV_CACHE_FP8) x = bf16_of_fp8(uint2{pool[row * D + d], 0}, code).x;
+    else x = bf16_of_fp4(pool[row * (D / 2) + d / 2] >> (4 * (d & 1)), code).x;
+    return __uint_as_float(x << 16);
   }
 }
 
 template <int DT, int FMT, int D>
-hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, hipStream_t s) {
-  const int64_t grid = (int64_t)c.S * c.max_new * qs.nh;
-  if (grid == 0) return hipSuccess;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  k_cache_attn_row<DT, FMT, D><<<(unsigned)grid, 64, 0, s>>>(c, mask, bank, qs);
+__global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mask mask, BankRows bank, CacheQueries qs,
+                                                                   int nrb, int nsplit, Part part) {
+  constexpr bool BF = DT == DKV_BF16, FULL = FMT == DKV_CACHE_FULL;
+  constexpr int TB = kFK * 2 * D;  // one bf16 tile of K or V
+  // Stages of (K tile, V tile) per wave; the first holds the waves' results at the end (32 rows of D floats).
+  // Two arrays, so that reads of one are known not to wait for loads into the other.
+  __shared__ __attribute__((aligned(1024))) char st0[kFWaves * 2 * TB], st1[BF && FULL ? kFWaves * 2 * TB : 16];
+  __shared__ float2 wml[kFWaves][32];
+  const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
+  const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
+  const int rb = p % nrb, bs = p / nrb, b = bs / nsplit, split = bs % nsplit;
+  const int s = b / c.H, h = b % c.H;
+  const NewRows nr = new_rows(c, s);
+  const int nrows = min(nr.n, c.max_new) * qs.G, r0 = rb * 32;
+  if (r0 >= nrows) return;
+  const int len = seq_length(c, s);
+  const int here = min(32, nrows - r0);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
+  const RowAt at = row_at(nr, qs, h, r0 + min(n, here - 1));
+  WaveMask wm;
+  wm.sink = mask.sink;
+  wm.row = seen_by(mask, len, nr.n, at.i);
+  wm.first = seen_by(mask, len, nr.n, r0 / qs.G);
+  wm.last = seen_by(mask, len, nr.n, (r0 + here - 1) / qs.G);
+  const Plan pl = plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G);
+  const int used = splits_used<kFLeast>(pl.total, nsplit);
+  if (split >= used) return;
+  int tb, nt;
+  split_range(pl.total, used, split, tb, nt);
+  PageWindow pw;
+  pw.init(c, s);
+  Rows<D> rows;
+  rows.init();
+  constexpr int EB = BF ? 2 : 4;  // bytes of a bank element
+  const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (EB * D);
+  const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (EB * D);
+  char *mine = st0 + wave * 2 * TB, *other = st1 + (BF && FULL ? wave * 2 * TB : 0);
+  if constexpr (BF) {
+    bf16x8 qf[D / 16];
+    load_q<D>(qf, qs, at, n < here);
+    auto compute = [&](int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
+      const bool isbank = t < pl.nb;
+      const int pos = tile_pos(pl, kFK, t);
+      f32x16 sc[1];
+      uint32_t pb[1][8];
+      scores<D, 1>(kt, qf, sc);
+      uint64_t vis = 0;
+      bool whole = true;
+      if (isbank) {
+        const int nv = pl.m - t * kFK;
+        if (nv < kFK) mask_bank<1>(sc, nv);
+        rows.any = true;
+      } else if (present == ~0ull && wm.all(pos, kFK)) {
+        rows.any = true;
+      } else {
+        whole = false;
+        vis = visible_bits(wm, pos, present);
+        rows.any |= mask_cache<1>(sc, vis);
+      }
+      softmax_update<D, 1>(rows, sc, pb, qs.scale_log2);
+      if (!whole) purge<D, 1, 64>(rows, vt, vis, true);
+      product<D, 1>(rows, pb, vt);
+    };
+    if constexpr (FULL) {
+      const Rows8<D> ld = rows8_offsets<D>();
+      auto issue = [&](int t, char *buf) -> uint64_t {
+        if (t >= nt) return 0;
+        if (t < pl.nb) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int r8 = t * kFK + 8 * g;
+            rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8), 8 * g, buf, buf + TB);
+          }
+          return ~0ull;
+        }
+        const int pos = tile_pos(pl, kFK, t);
+        pw.seek(pos >> c.lps);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
+          int nv = bound(pl.hi - p8, 0, 8);
+          if (page < 0 || (p8 + 8 <= pl.lo && p8 >= mask.sink)) nv = 0;
+          const size_t row = pool_row(c, page < 0 ? 0 : page, h, p8);
+          rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * g, buf, buf + TB);
+        }
+        return present_keys<kFK>(pw, pos, c.lps);
+      };
+      constexpr int kTileLoads = 4 * 2 * Rows8<D>::kLoads;
+      auto step = [&](int t, char *buf, uint64_t present, char *next) __attribute__((always_inline)) {
+        const uint64_t nx = issue(t + kFWaves, next);
+        // this tile's loads are done, the next one's may be on their way
+        if (t + kFWaves < nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
+        else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+        asm volatile("" ::: "memory");
+        compute(t, buf, buf + TB, present);
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
+        asm volatile("" ::: "memory");
+        return nx;
+      };
+      uint64_t p0 = issue(tb + wave, mine), p1 = 0;
+      for (int t = tb + wave; t < nt; t += 2 * kFWaves) {
+        p1 = step(t, mine, p0, other);
+        if (t + kFWaves < nt) p0 = step(t + kFWaves, other, p1, mine);
+      }
+    } else {
+      // a lane: two quarter rows of K and two of V, in rows l / 4 and 16 + l / 4
+      Quarter<FMT, D> xk[2], xv[2];
+      const int part4 = l & 3;
+      uint64_t pcur = 0, pnext = 0;
+      bool bnext = false;
+      auto fetch = [&](int t) {
+        if (t >= nt) return;
+        bnext = t < pl.nb;
+        if (bnext) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int slot = t * kFK + 16 * g + (l >> 2);
+            xk[g].load_bank(reinterpret_cast<const uint16_t *>(bk) + (size_t)slot * D, part4, slot < pl.m);
+            xv[g].load_bank(reinterpret_cast<const uint16_t *>(bv) + (size_t)slot * D, part4, slot < pl.m);
+          }
+          pnext = ~0ull;
+          return;
+        }
+        const int pos = tile_pos(pl, kFK, t);
+        pw.seek(pos >> c.lps);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int p16 = pos + 16 * g, at_pos = p16 + (l >> 2), page = pw.page(p16 >> c.lps);
+          const bool ok = page >= 0 && at_pos < pl.hi && (p16 + 16 > pl.lo || p16 < mask.sink);
+          const size_t row = pool_row(c, page < 0 ? 0 : page, h, at_pos);
+          xk[g].load(c.k, c.ks, row, part4, ok);
+          xv[g].load(c.v, c.vs, row, part4, ok);
+        }
+        pnext = present_keys<kFK>(pw, pos, c.lps);
+      };
+      fetch(tb + wave);
+      for (int t = tb + wave; t < nt; t += kFWaves) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          xk[g].template store<false>(mine, 16 * g + (l >> 2), part4, bnext);
+          xv[g].template store<true>(mine + TB, 16 * g + (l >> 2), part4, bnext);
+        }
+        pcur = pnext;
+        fetch(t + kFWaves);
+        __builtin_amdgcn_wave_barrier();  // one wave: its LDS operations run in order
+        compute(t, mine, mine + TB, pcur);
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  } else {
+    constexpr int KC = D / 8;
+    float4 qf[KC];
+    {
+      const float *q = static_cast<const float *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh;
+#pragma unroll
+      for (int k = 0; k < KC; ++k) qf[k] = *reinterpret_cast<const float4 *>(q + 8 * k + 4 * lh);
+    }
+    auto tile = [&](auto fmt, int t, const unsigned char *kp, const uint8_t *ks, const unsigned char *vp, const uint8_t *vs,
+                    auto row_of, uint32_t okbits) __attribute__((always_inline)) {
+      // okbits: rows of the tile that may be read; the others count as zeros
+      constexpr int F = decltype(fmt)::value;
+      const int pos = tile_pos(pl, kFK, t);
+      const bool kok = (okbits >> n) & 1;
+      const size_t krow = row_of(n);
+      f32x16 sc = {};
+#pragma unroll
+      for (int k = 0; k < KC; ++k) {
+        float4 kx = {0, 0, 0, 0};
+        if (kok) kx = load_f32x4<F, D>(kp, ks, krow, 8 * k + 4 * lh);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.x, qf[k].x, sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.y, qf[k].y, sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.z, qf[k].z, sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.w, qf[k].w, sc, 0, 0, 0);
+      }
+      uint32_t vis = 0;
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
+        const bool ok = ((okbits >> k) & 1) && (t < pl.nb || sees(wm.row, wm.sink, pos + k));
+        if (ok) vis |= 1u << i;
+        sc[i] = ok ? sc[i] * qs.scale_log2 : -INFINITY;
+        tmax = fmaxf(tmax, sc[i]);
+      }
+      rows.any |= vis != 0;
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+      const float mnew = fmaxf(rows.mrun, tmax);
+      const float mref = mnew == -INFINITY ? 0.0f : mnew;
+      const float corr = exp2f(rows.mrun - mref);
+      rows.mrun = mnew;
+      float pw_[16], ps = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        pw_[i] = exp2f(sc[i] - mref);
+        ps += pw_[i];
+      }
+      rows.lrun = __builtin_fmaf(rows.lrun, corr, ps);
+#pragma unroll
+      for (int t2 = 0; t2 < D / 32; ++t2) {
+        float vx[16];
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
+          vx[i] = (okbits >> k) & 1 ? load_f32<F, D>(vp, vs, row_of(k), 32 * t2 + n) : 0.0f;
+          bad |= (__float_as_uint(vx[i]) & 0x7f800000u) == 0x7f800000u;
+        }
+        rows.o[t2] *= corr;
+        if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it
+          f32x16 kinds = {};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t u = __float_as_uint(vx[i]);
+            const float kind = (u & 0x7fffffffu) < 0x7f800000u ? 0.0f : ((u & 0x7fffffffu) > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
+            kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> i) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
+            if (kind != 0.0f) vx[i] = 0.0f;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[i], pw_[i], rows.o[t2], 0, 0, 0);
+      }
+    };
+    for (int t = tb + wave; t < nt; t += kFWaves) {
+      if (t < pl.nb) {
+        const int nv = min(kFK, pl.m - t * kFK);
+        tile(std::integral_constant<int, DKV_CACHE_FULL>(), t, bk, nullptr, bv, nullptr,
+             [&](int k) { return (size_t)t * kFK + k; }, nv >= 32 ? 0xffffffffu : (1u << nv) - 1u);
+        continue;
+      }
+      const int pos = tile_pos(pl, kFK, t);
+      pw.seek(pos >> c.lps);
+      const int pa = pw.page(pos >> c.lps), pb = pw.page((pos + 16) >> c.lps);
+      uint32_t okbits = (pa >= 0 ? 0xffffu : 0u) | (pb >= 0 ? 0xffff0000u : 0u);
+      if (pl.hi - pos < 32) okbits &= (1u << (pl.hi - pos)) - 1u;
+      // rows before the window of every row block's token and behind the first tokens are not read
+      tile(std::integral_constant<int, FMT>(), t, c.k, c.ks, c.v, c.vs,
+           [&](int k) { return pool_row(c, max(k < 16 ? pa : pb, 0), h, pos + k); }, okbits);
+    }
+  }
+
+  // the four waves' results, joined under their common maximum (bf16: of raw scores)
+  const float unit = BF ? qs.scale_log2 : 1.0f;
+  const bool any = either_half(rows.any);
+  const float lw = row_sum(rows.mrun, rows.lrun + __shfl_xor(rows.lrun, 32, 64), any);
+  float *mo = reinterpret_cast<float *>(mine);
+  if (n < here) {
+    if (lh == 0) wml[wave][n] = float2{rows.mrun, lw};
+#pragma unroll
+    for (int t2 = 0; t2 < D / 32; ++t2)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4 *>(mo + n * D + 4 * ((8 * t2 + 2 * g + lh) ^ (n % 8))) =
+            float4{rows.o[t2][4 * g], rows.o[t2][4 * g + 1], rows.o[t2][4 * g + 2], rows.o[t2][4 * g + 3]};
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * kFWaves) {
+    const int rr = e / (D / 4), j = 4 * (e % (D / 4));
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kFWaves; ++w) M = fmaxf(M, wml[w][rr].x);
+    float lt = 0.0f, a[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kFWaves; ++w) {
+      const float2 ml = wml[w][rr];
+      const float f = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
+      const float4 x = *reinterpret_cast<const float4 *>(st0 + w * 2 * TB + 4 * (rr * D + (j ^ (4 * (rr % 8)))));
+      lt = __builtin_fmaf(ml.y, f, lt);
+      a[0] = __builtin_fmaf(x.x, f, a[0]);
+      a[1] = __builtin_fmaf(x.y, f, a[1]);
+      a[2] = __builtin_fmaf(x.z, f, a[2]);
+      a[3] = __builtin_fmaf(x.w, f, a[3]);
+    }
+    const RowAt ra = row_at(nr, qs, h, r0 + rr);
+    if (part.ml) {
+      const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
+      const size_t row = (size_t)split * nrow + ((size_t)s * c.max_new + ra.i) * qs.nh + ra.hq;
+      if (j == 0) part.ml[row] = float2{M, lt};
+      *reinterpret_cast<float4 *>(part.o + row * D + j) = float4{a[0], a[1], a[2], a[3]};
+      continue;
+    }
+    const float inv = inv_sum(lt);
+    const size_t o = ra.t * qs.ot + (size_t)ra.hq * qs.oh + j;
+    if constexpr (BF)
+      *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(qs.out) + o) =
+          u32x2{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
+    else
+      *reinterpret_cast<float4 *>(static_cast<float *>(qs.out) + o) = float4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+  }
+}
+
+// Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  D / 4 lanes
+// per row; RB rows per row block, KT keys per tile of the kernel that wrote them.
+template <int DT, int D, int RB, int KT, int LEAST>
+__global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit,
+                                                       Part part) {
+  constexpr int LR = D / 4;
+  const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
+  const size_t row = (size_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
+  const int j = 4 * (threadIdx.x % LR);
+  if (row >= nrow) return;
+  const unsigned per = (unsigned)c.max_new * qs.nh;  // < 2^31
+  const int s = (int)(row / per);
+  const unsigned rest = (unsigned)(row - (size_t)s * per);
+  const int i = (int)(rest / (unsigned)qs.nh), hq = (int)(rest % (unsigned)qs.nh), h = hq / qs.G;
+  const float2 ml0 = part.ml[row];  // read while the plan is on its way
+  const float4 x0 = *reinterpret_cast<const float4 *>(part.o + row * D + j);
+  const NewRows nr = new_rows(c, s);
+  const int n = min(nr.n, c.max_new);
+  if (i >= n) return;
+  const int r0 = (i * qs.G + hq - h * qs.G) / RB * RB, r1 = min(r0 + RB, n * qs.G) - 1;
+  const Plan pl = plan_of<KT>(mask, bank, s * c.H + h, seq_length(c, s), nr.n, r0 / qs.G, r1 / qs.G);
+  const int used = splits_used<LEAST>(pl.total, nsplit);
+  const float unit = DT == DKV_BF16 ? qs.scale_log2 : 1.0f;  // the bf16 maxima are raw scores
+  float M = ml0.x;
+  for (int k = 1; k < used; ++k) M = fmaxf(M, part.ml[k * nrow + row].x);
+  const float w0 = ml0.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml0.x - M) * unit);
+  float l = ml0.y * w0, a[4] = {x0.x * w0, x0.y * w0, x0.z * w0, x0.w * w0};
+  for (int k = 1; k < used; ++k) {
+    const float2 ml = part.ml[k * nrow + row];
+    const float4 x = *reinterpret_cast<const float4 *>(part.o + (k * nrow + row) * D + j);
+    const float w = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
+    l = __builtin_fmaf(ml.y, w, l);
+    a[0] = __builtin_fmaf(x.x, w, a[0]);
+    a[1] = __builtin_fmaf(x.y, w, a[1]);
+    a[2] = __builtin_fmaf(x.z, w, a[2]);
+    a[3] = __builtin_fmaf(x.w, w, a[3]);
+  }
+  const float inv = inv_sum(l);
+  const size_t o = (size_t)(nr.first + i) * qs.ot + (size_t)hq * qs.oh + j;
+  if constexpr (DT == DKV_BF16)
+    *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(qs.out) + o) =
+        u32x2{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
+  else
+    *reinterpret_cast<float4 *>(static_cast<float *>(qs.out) + o) = float4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+}
+
+constexpr int kCUs = 256;
+constexpr int kMaxSplit = 64;
+constexpr int kFewRows = 64;  // rows of a (sequence, kv head) up to which 32-row blocks are taken
+
+bool takes_few(const Pages &c, int dtype, int G) { return dtype != DKV_BF16 || (long long)c.max_new * G <= kFewRows; }
+
+template <int DT, int FMT, int D>
+hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, void *ws, int nsplit,
+                     hipStream_t s) {
+  const int64_t nrow = (int64_t)c.S * c.max_new * qs.nh;
+  if (nrow == 0) return hipSuccess;
+  Part part{nullptr, nullptr};
+  if (nsplit > 1) {  // the outputs first, then the maxima and sums
+    part.o = static_cast<float *>(ws);
+    part.ml = reinterpret_cast<float2 *>(part.o + nrow * nsplit * D);
+  }
+  const bool few = takes_few(c, DT, qs.G);
+  const int64_t nrb = ((int64_t)c.max_new * qs.G + (few ? 31 : kWRows - 1)) / (few ? 32 : kWRows);
+  const int64_t grid = nrb * c.S * c.H * nsplit;
+  constexpr int kRows = 256 / (D / 4);
+  const int64_t cgrid = (nrow + kRows - 1) / kRows;
+  if (grid > 0x7fffffffLL || cgrid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (few) {
+    k_cache_attn_few<DT, FMT, D><<<(unsigned)grid, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+    if (nsplit > 1)
+      k_cache_combine<DT, D, 32, kFK, kFLeast><<<(unsigned)cgrid, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
+  } else if constexpr (DT == DKV_BF16) {
+    k_cache_attn_wide<FMT, D><<<(unsigned)grid, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+    if (nsplit > 1)
+      k_cache_combine<DT, D, kWRows, kWK, kWLeast><<<(unsigned)cgrid, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-int cache_attention_splits(const Pages &, int, int, int, const Mask &, const BankRows &, int, size_t *bytes) {
+// Splits: the time is about rounds of workgroups over the chip times (tiles per split and
+// some tiles' worth of prologue), plus the joining kernel.
+int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask &mask, const BankRows &bank, int nh,
+                           size_t *bytes) {
   *bytes = 0;
-  return 1;
+  const int G = nh / c.H;
+  const int64_t nrow = (int64_t)c.S * c.max_new * nh;
+  if (nrow == 0) return 1;
+  const bool few = takes_few(c, dtype, G);
+  const int KT = few ? kFK : kWK, RB = few ? 32 : kWRows, least = few ? kFLeast : kWLeast;
+  int64_t keys = (int64_t)c.cols << c.lps;
+  if (mask.window > 0) {
+    const int64_t seen = (int64_t)mask.window + (mask.causal ? c.max_new : 0) + mask.sink + KT;
+    if (seen < keys) keys = seen;
+  }
+  const int64_t tiles = (keys + KT - 1) / KT + (bank.cap + KT - 1) / KT;
+  const int64_t nwg = ((int64_t)c.max_new * G + RB - 1) / RB * c.S * c.H;
+  const int64_t slots = few && (dtype != DKV_BF16 || fmt != DKV_CACHE_FULL) ? 2 * kCUs : kCUs;
+  const double each = few ? kFWaves : 1;  // tiles walked at a time
+  int best = 1;
+  double best_cost = 0.0;
+  for (int S = 1; S <= kMaxSplit && (S == 1 || tiles / S >= least); ++S) {
+    const double rounds = (double)((nwg * S + slots - 1) / slots);
+    double cost = rounds * ((double)((tiles + S - 1) / S) / each + 6);
+    if (S > 1) cost += 4.0 + (double)nrow * S * (8.0 * d + 16.0) / (4e12 * 1.6e-6);
+    if (S == 1 || cost < 0.95 * best_cost) best = S, best_cost = cost;
+  }
+  if (best > 1) *bytes = (size_t)nrow * best * (d * 4 + 8);
+  return best;
 }
 
 hipError_t launch_cache_attention(const Pages &c, int dtype, int fmt, int d, const Mask &mask, const BankRows &bank,
-                                  const CacheQueries &qs, void *, int, hipStream_t s) {
+                                  const CacheQueries &qs, void *ws, int nsplit, hipStream_t s) {
 #define DKV_CASE(DT, FMT, D) \
-  if (dtype == DT && fmt == FMT && d == D) return attn_impl<DT, FMT, D>(c, mask, bank, qs, s);
+  if (dtype == DT && fmt == FMT && d == D) return attn_impl<DT, FMT, D>(c, mask, bank, qs, ws, nsplit, s);
   DKV_CASE(DKV_BF16, DKV_CACHE_FULL, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FULL, 128)
   DKV_CASE(DKV_BF16, DKV_CACHE_FP8, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FP8, 128)
   DKV_CASE(DKV_BF16, DKV_CACHE_FP4, 64) DKV_CASE(DKV_BF16, DKV_CACHE_FP4, 128)
