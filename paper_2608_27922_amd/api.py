@@ -458,6 +458,7 @@ class PagedCache:
                                       for _ in range(2))
         self.page_table = torch.full((num_seqs, max_pages), -1, dtype=torch.int32, device=dev)
         self.length = torch.zeros(num_seqs, dtype=torch.int32, device=dev)
+        self._index = self.k.device.index
         self._c = DkvCache(num_seqs, num_kv_heads, head_dim, page_size, num_pages, max_pages, _dtype_code(dtype),
                            CACHE_FORMATS[format], self.k.data_ptr(), self.v.data_ptr(), _ptr(self.k_scale),
                            _ptr(self.v_scale), self.page_table.data_ptr(), self.length.data_ptr())
@@ -493,28 +494,40 @@ def _chunk(cache: PagedCache, T: int, start: Optional[torch.Tensor], max_new: Op
 
 
 def _check_rows(cache: PagedCache, t: torch.Tensor, what: str):
-    """[T, heads, d] in the cache's dtype and on its device, unit stride within a row; the strides of a token and a head."""
-    if t.dim() != 3 or t.shape[2] != cache.d or t.dtype != cache.dtype or t.device != cache.k.device:
+    """[T, heads, d] in the cache's dtype and on its device, unit stride within a row; the strides of a token and a head
+    and the address."""
+    s, p = t.shape, t.data_ptr()
+    if len(s) != 3 or s[2] != cache.d or t.dtype != cache.dtype or t.device != cache.k.device:
         raise ValueError(f"{what} must be [tokens, heads, head_dim] in the cache's dtype, on its device")
     st = t.stride()
-    if st[2] != 1 or (st[0] | st[1]) % (16 // t.element_size()) or t.data_ptr() % 16:
+    if st[2] != 1 or (st[0] | st[1]) % (16 // t.element_size()) or p % 16:
         raise ValueError(f"the rows of {what} must be contiguous and start at multiples of 16 bytes")
-    return st[0], st[1]
+    return s, st, p
+
+
+def _enqueue(cache: PagedCache, where: str, fn, *args):
+    """fn(*args, stream) on the current stream of the cache's device, which need not be the current device."""
+    i = cache._index
+    if torch.cuda.current_device() == i:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(i))
+    _check(status, where)
 
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
                 max_new: Optional[int] = None):
     """densitykv_cache_write: the new rows k, v [T, num_kv_heads, d] into their pages, on the current stream.
     `start` [S + 1]: first row of each sequence (None: T / S rows each); `max_new`: a bound of the rows of a sequence."""
-    st = _check_rows(cache, k, "k")
-    if k.shape[1] != cache.H or v.shape != k.shape:
+    shape, st, pk = _check_rows(cache, k, "k")
+    vshape, vst, pv = _check_rows(cache, v, "v")
+    if shape[1] != cache.H or vshape != shape:
         raise ValueError("k and v must be [tokens, num_kv_heads, head_dim]")
-    if _check_rows(cache, v, "v") != st:
+    if vst != st:
         raise ValueError("k and v must have the same strides")
-    cc, ch = cache.c(), _chunk(cache, int(k.shape[0]), start, max_new)
-    with torch.cuda.device(cache.k.device):
-        _check(lib().densitykv_cache_write(ctypes.byref(cc), ctypes.byref(ch), _ptr(k), _ptr(v), st[0], st[1], _stream()),
-               "cache_write")
+    _enqueue(cache, "cache_write", lib().densitykv_cache_write, ctypes.byref(cache.c()),
+             ctypes.byref(_chunk(cache, shape[0], start, max_new)), pk, pv, st[0], st[1])
 
 
 def cache_read(cache: PagedCache, n: int, first: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
@@ -529,12 +542,10 @@ def cache_read(cache: PagedCache, n: int, first: Optional[torch.Tensor] = None, 
     shape = (cache.S * cache.H, n, cache.d)
     k, v = (torch.empty(shape, dtype=cache.dtype, device=cache.k.device) if t is None else t for t in (k, v))
     for t in (k, v):
-        if tuple(t.shape) != shape or t.dtype != cache.dtype or not t.is_contiguous() or t.device != cache.k.device:
+        if t.shape != shape or t.dtype != cache.dtype or not t.is_contiguous() or t.device != cache.k.device:
             raise ValueError("k and v must be contiguous [num_seqs * num_kv_heads, n, head_dim] tensors in the cache's dtype")
-    cc = cache.c()
-    with torch.cuda.device(cache.k.device):
-        _check(lib().densitykv_cache_read(ctypes.byref(cc), _ptr(first), n, _ptr(k), _ptr(v), _stream()),
-               "cache_read")
+    _enqueue(cache, "cache_read", lib().densitykv_cache_read, ctypes.byref(cache.c()), _ptr(first), n, k.data_ptr(),
+             v.data_ptr())
     return k, v
 
 
@@ -544,32 +555,34 @@ def cache_attention(cache: PagedCache, q: torch.Tensor, start: Optional[torch.Te
                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """densitykv_cache_attention: q [T, num_heads, d] of the new tokens over [bank; cache]; each sees (causal) the tokens
     up to its own position, of those the last `window` (0: all) and the first `n_sink`.  The partial results of a split call
-    are in `workspace` (uint8) if it is given, else in a buffer of the caching allocator, held for the call."""
-    qt, qh = _check_rows(cache, q, "q")
-    T, nh = int(q.shape[0]), int(q.shape[1])
+    are in `workspace` (on the cache's device) if it is given, else in a buffer of the caching allocator, held for the call."""
+    shape, st, pq = _check_rows(cache, q, "q")
     if out is None:  # a ragged chunk may leave rows without a sequence
-        out = (torch.zeros if start is not None else torch.empty)(T, nh, cache.d, dtype=q.dtype, device=q.device)
-    elif out.shape != q.shape:
+        out = (torch.zeros if start is not None else torch.empty)(shape, dtype=q.dtype, device=q.device)
+    oshape, ost, po = _check_rows(cache, out, "out")
+    if oshape != shape:
         raise ValueError("out must have the shape of q")
-    ot, oh = _check_rows(cache, out, "out")
     scale = (1.0 / cache.d ** 0.5) if softmax_scale is None else float(softmax_scale)
-    if bank is not None and bank.k.device != cache.k.device:
-        raise ValueError("the bank must be on the cache's device")
-    L, cc, ch = lib(), cache.c(), _chunk(cache, T, start, max_new)
-    cq = DkvCacheQueries(nh, _i32(window, "window"), _i32(n_sink, "n_sink"), 1 if causal else 0, scale, qt, qh, ot, oh)
-    pc, pch, pq, pb = ctypes.byref(cc), ctypes.byref(ch), ctypes.byref(cq), None
+    L = lib()
+    pc, pch = ctypes.byref(cache.c()), ctypes.byref(_chunk(cache, shape[0], start, max_new))
+    cq = ctypes.byref(DkvCacheQueries(_i32(shape[1], "the number of heads"), _i32(window, "window"), _i32(n_sink, "n_sink"),
+                                      1 if causal else 0, scale, st[0], st[1], ost[0], ost[1]))
+    pb = None
     if bank is not None:
-        cb = bank.c()
-        pb = ctypes.byref(cb)
-    size = ctypes.c_size_t(0)
-    with torch.cuda.device(cache.k.device):
-        if workspace is None:
-            _check(L.densitykv_cache_attention_workspace_size(pc, pch, pb, pq, ctypes.byref(size)), "cache_attention")
-            if size.value:
-                workspace = torch.empty(size.value, dtype=torch.uint8, device=q.device)
-        _check(L.densitykv_cache_attention(pc, pch, pb, pq, _ptr(q), _ptr(out), _ptr(workspace),
-                                           0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                           _stream()), "cache_attention")
+        if bank.k.device != cache.k.device:
+            raise ValueError("the bank must be on the cache's device")
+        pb = ctypes.byref(bank.c())
+    nbytes = 0
+    if workspace is None:
+        size = ctypes.c_size_t(0)
+        _check(L.densitykv_cache_attention_workspace_size(pc, pch, pb, cq, ctypes.byref(size)), "cache_attention")
+        if size.value:
+            workspace = torch.empty(size.value, dtype=torch.uint8, device=q.device)
+    elif not workspace.is_contiguous() or workspace.device != cache.k.device:
+        raise ValueError("workspace must be contiguous, on the cache's device")
+    if workspace is not None:
+        nbytes = workspace.numel() * workspace.element_size()
+    _enqueue(cache, "cache_attention", L.densitykv_cache_attention, pc, pch, pb, cq, pq, po, _ptr(workspace), nbytes)
     return out
 
 
