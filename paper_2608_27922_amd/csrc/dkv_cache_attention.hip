@@ -149,15 +149,8 @@ __device__ __forceinline__ void rows8_issue(int rsub, int pc, const int *voff, c
 // A quarter row (D / 4 elements) on its way from memory to an LDS tile through registers.
 template <int FMT, int D>
 struct Quarter {
-  u32x4 x[D / 32];  // bank rows take all of it, FP8 rows half, FP4 rows a quarter
+  u32x4 x[FMT == DKV_CACHE_FP8 ? D / 64 : 1];
   int code;
-  __device__ __forceinline__ void load_bank(const uint16_t *row, int part, bool ok) {
-#pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-      x[e] = u32x4{0, 0, 0, 0};
-      if (ok) x[e] = *reinterpret_cast<const u32x4 *>(row + part * (D / 4) + 8 * e);
-    }
-  }
   __device__ __forceinline__ void load(const unsigned char *pool, const uint8_t *scale, size_t row, int part, bool ok) {
     code = kScaleBias;
     x[0] = u32x4{0, 0, 0, 0};
@@ -182,12 +175,11 @@ struct Quarter {
     if (ok) code = scale[row * (D / kGroup) + part * (D / 4) / kGroup];
   }
   template <bool V>
-  __device__ __forceinline__ void store(char *tile, int r, int part, bool bank) const {
+  __device__ __forceinline__ void store(char *tile, int r, int part) const {
 #pragma unroll
     for (int e = 0; e < D / 32; ++e) {
       uint4 y;
-      if (bank) y = uint4{x[e][0], x[e][1], x[e][2], x[e][3]};
-      else if constexpr (FMT == DKV_CACHE_FP8) y = bf16_of_fp8(uint2{x[e / 2][2 * (e & 1)], x[e / 2][2 * (e & 1) + 1]}, code);
+      if constexpr (FMT == DKV_CACHE_FP8) y = bf16_of_fp8(uint2{x[e / 2][2 * (e & 1)], x[e / 2][2 * (e & 1) + 1]}, code);
       else y = bf16_of_fp4(x[0][e], code);
       const int ch = part * (D / 32) + e;
       *reinterpret_cast<uint4 *>(tile + r * (2 * D) + 16 * (V ? v_swz<D>(r, ch) : k_swz<D>(r, ch))) = y;
@@ -241,6 +233,14 @@ __device__ __forceinline__ void scores(const char *kt, const bf16x8 *qf, f32x16 
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[kk], qf[kk], acc, 0, 0, 0);
     sc[sub] = acc;
+  }
+  // LDS fragment reads run 6 MFMAs ahead of their use
+  constexpr int N = NSUB * D / 16, A = N < 6 ? N : 6;
+  __builtin_amdgcn_sched_group_barrier(0x100, A, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i + A < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
 }
 
@@ -329,6 +329,14 @@ __device__ __forceinline__ void product(Rows<D> &r, const uint32_t (*pb)[8], con
         r.o[t2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_operand<D>(vt, sub, kst, t2)),
                                                           __builtin_bit_cast(bf16x8, bp), r.o[t2], 0, 0, 0);
     }
+  }
+  // the two transposed reads of an MFMA run 4 MFMAs ahead of it
+  constexpr int N = 2 * NSUB * D / 32, A = N < 4 ? N : 4;
+  __builtin_amdgcn_sched_group_barrier(0x100, 2 * A, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i + A < N) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
   }
 }
 
@@ -501,8 +509,8 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   int tb, nt;
   split_range(pl.total, used, split, tb, nt);
 
-  __shared__ __attribute__((aligned(1024))) char k0[TB], k1[TB], k2[FULL ? TB : 16];
-  __shared__ __attribute__((aligned(1024))) char v0[TB], v1[TB], v2[FULL ? TB : 16];
+  __shared__ __attribute__((aligned(1024))) char k0[TB], k1[TB], k2[TB];
+  __shared__ __attribute__((aligned(1024))) char v0[TB], v1[TB], v2[TB];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
   const int w0 = r0 + 32 * wave;
   const bool work = w0 < nrows;  // a wave past the last row only loads
@@ -525,8 +533,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (2 * D);
 
   const Seen bfirst = seen_by(mask, len, nr.n, r0 / qs.G), blast = seen_by(mask, len, nr.n, r1 / qs.G);
-  auto compute = [&](int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
-    const bool isbank = t < pl.nb;
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
     const int pos = tile_pos(pl, kWK, t);
     const bool act = work && (isbank || !wm.none(pos, kWK));
     // whether every row of the workgroup sees all of the tile: the same for all its waves
@@ -552,16 +559,17 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     if (act) product<D, 2>(rows, pb, vt);
   };
 
-  if constexpr (FULL) {
-    // K and V tiles go global -> LDS without registers, three stages: two tiles in flight
-    // while one is used.  A wave loads 8 rows of each tile, which lie in one page.
-    const Rows8<D> ld = rows8_offsets<D>();
+  // Tiles [t0, t1) of rows held in bf16 go global -> LDS without registers, three stages: two
+  // tiles in flight while one is used.  A wave loads 8 rows of each tile, which lie in one page.
+  const Rows8<D> ld = rows8_offsets<D>();
+  auto run_direct = [&](int t0, int t1) __attribute__((always_inline)) {
     uint64_t pr[3] = {0, 0, 0};
     auto issue = [&](int t, char *kd, char *vd) -> uint64_t {
-      if (t >= nt) return 0;
-      if (t < pl.nb) {
+      if (t >= t1) return 0;
+      if (!FULL || t < pl.nb) {
         const int r8 = t * kWK + 8 * wave;
-        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8), 8 * wave, kd, vd);
+        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8),
+                       8 * wave, kd, vd);
         return ~0ull;
       }
       const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
@@ -575,71 +583,78 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     };
     constexpr int kTileLoads = 2 * Rows8<D>::kLoads;
     auto step = [&](int t, const char *kt, char *vt, uint64_t present, char *kn, char *vn) __attribute__((always_inline)) {
-      if (t + 1 < nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
+      if (t + 1 < t1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
       else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
       stage_barrier();
       const uint64_t nx = issue(t + 2, kn, vn);
-      compute(t, kt, vt, present);
+      compute(!FULL || t < pl.nb, t, kt, vt, present);
       return nx;
     };
-    pr[0] = issue(tb, k0, v0);
-    pr[1] = issue(tb + 1, k1, v1);
-    for (int t = tb; t < nt; t += 3) {
+    pr[0] = issue(t0, k0, v0);
+    pr[1] = issue(t0 + 1, k1, v1);
+    for (int t = t0; t < t1; t += 3) {
       pr[2] = step(t, k0, v0, pr[0], k2, v2);
-      if (t + 1 < nt) pr[0] = step(t + 1, k1, v1, pr[1], k0, v0);
-      if (t + 2 < nt) pr[1] = step(t + 2, k2, v2, pr[2], k1, v1);
+      if (t + 1 < t1) pr[0] = step(t + 1, k1, v1, pr[1], k0, v0);
+      if (t + 2 < t1) pr[1] = step(t + 2, k2, v2, pr[2], k1, v1);
     }
+  };
+  if constexpr (FULL) {
+    run_direct(tb, nt);
   } else {
-    // Quantised rows come through registers and are stored as bf16: waves 0-3 a quarter row
-    // of K per lane, waves 4-7 of V, each wave 16 rows that lie in one page.
+    const int t0 = max(tb, min(nt, pl.nb));
+    if (tb < t0) {
+      run_direct(tb, t0);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      stage_barrier();
+    }
+    // Quantised rows come through registers, two tiles ahead, and are stored as bf16: waves 0-3
+    // a quarter row of K per lane, waves 4-7 of V, each wave 16 rows that lie in one page.  Of
+    // the two waves of a SIMD one converts before its matrix work and one after it.
     const bool isv = wave >= 4;
     const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
-    Quarter<FMT, D> x;
-    uint64_t pcur = 0, pnext = 0;
-    bool bnext = false;
-    auto fetch = [&](int t) {
+    struct {
+      Quarter<FMT, D> x;
+      uint64_t present;
+    } f[2];
+    auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
       if (t >= nt) return;
-      bnext = t < pl.nb;
-      if (bnext) {
-        const int slot = t * kWK + lr;
-        x.load_bank(reinterpret_cast<const uint16_t *>(isv ? bv : bk) + (size_t)slot * D, qpart, slot < pl.m);
-        pnext = ~0ull;
-        return;
-      }
       const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
       pw.seek(pos >> c.lps);
       const int page = pw.page(p16 >> c.lps);
       const bool ok = page >= 0 && pos + lr < pl.hi && (p16 + 16 > pl.lo || p16 < mask.sink);
       const size_t row = pool_row(c, page < 0 ? 0 : page, h, pos + lr);
-      x.load(isv ? c.v : c.k, isv ? c.vs : c.ks, row, qpart, ok);
-      pnext = present_keys<kWK>(pw, pos, c.lps);
+      y.x.load(isv ? c.v : c.k, isv ? c.vs : c.ks, row, qpart, ok);
+      y.present = present_keys<kWK>(pw, pos, c.lps);
     };
-    auto put = [&](char *kd, char *vd) {
-      if (isv) x.template store<true>(vd, lr, qpart, bnext);
-      else x.template store<false>(kd, lr, qpart, bnext);
-    };
-    auto step = [&](int t, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
-      const uint64_t present = pcur;
-      if (t + 1 < nt) {
-        put(kn, vn);
-        pcur = pnext;
-        fetch(t + 2);
+    uint64_t present = 0;
+    auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
+      const uint64_t now = present, next = y.present;
+      if (!isv && t + 1 < nt) {
+        y.x.template store<false>(kn, lr, qpart);
+        fetch(y, t + 3);
       }
-      compute(t, kt, vt, present);
+      compute(false, t, kt, vt, now);
+      if (isv && t + 1 < nt) {
+        y.x.template store<true>(vn, lr, qpart);
+        fetch(y, t + 3);
+      }
+      present = next;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
       stage_barrier();
     };
-    if (tb < nt) {
-      fetch(tb);
-      put(k0, v0);
-      pcur = pnext;
-      fetch(tb + 1);
+    if (t0 < nt) {
+      fetch(f[0], t0);
+      fetch(f[1], t0 + 1);
+      if (isv) f[0].x.template store<true>(v0, lr, qpart);
+      else f[0].x.template store<false>(k0, lr, qpart);
+      present = f[0].present;
+      fetch(f[0], t0 + 2);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       stage_barrier();
     }
-    for (int t = tb; t < nt; t += 2) {
-      step(t, k0, v0, k1, v1);
-      if (t + 1 < nt) step(t + 1, k1, v1, k0, v0);
+    for (int t = t0; t < nt; t += 2) {
+      step(t, f[1], k0, v0, k1, v1);
+      if (t + 1 < nt) step(t + 1, f[0], k1, v1, k0, v0);
     }
   }
   if (!work) return;
@@ -709,7 +724,7 @@ __device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8
 }
 
 template <int DT, int FMT, int D>
-__global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mask mask, BankRows bank, CacheQueries qs,
+__global__ __launch_bounds__(64 * kFWaves, (DT == DKV_BF16 && FMT != DKV_CACHE_FULL) || D == 64 ? 2 : 1) void k_cache_attn_few(Pages c, Mask mask, BankRows bank, CacheQueries qs,
                                                                    int nrb, int nsplit, Part part) {
   constexpr bool BF = DT == DKV_BF16, FULL = FMT == DKV_CACHE_FULL;
   constexpr int TB = kFK * 2 * D;  // one bf16 tile of K or V
@@ -749,8 +764,7 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
   if constexpr (BF) {
     bf16x8 qf[D / 16];
     load_q<D>(qf, qs, at, n < here);
-    auto compute = [&](int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
-      const bool isbank = t < pl.nb;
+    auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
       const int pos = tile_pos(pl, kFK, t);
       f32x16 sc[1];
       uint32_t pb[1][8];
@@ -772,16 +786,21 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
       if (!whole) purge<D, 1, 64>(rows, vt, vis, true);
       product<D, 1>(rows, pb, vt);
     };
+    const Rows8<D> ld = rows8_offsets<D>();
+    auto issue_bank = [&](int t, char *buf) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int r8 = t * kFK + 8 * g;
+        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8),
+                       8 * g, buf, buf + TB);
+      }
+    };
     if constexpr (FULL) {
-      const Rows8<D> ld = rows8_offsets<D>();
+      // two stages: a tile in flight while the other is used
       auto issue = [&](int t, char *buf) -> uint64_t {
         if (t >= nt) return 0;
         if (t < pl.nb) {
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int r8 = t * kFK + 8 * g;
-            rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8), 8 * g, buf, buf + TB);
-          }
+          issue_bank(t, buf);
           return ~0ull;
         }
         const int pos = tile_pos(pl, kFK, t);
@@ -803,7 +822,7 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
         if (t + kFWaves < nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
         else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
         asm volatile("" ::: "memory");
-        compute(t, buf, buf + TB, present);
+        compute(t < pl.nb, t, buf, buf + TB, present);
         __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
         asm volatile("" ::: "memory");
         return nx;
@@ -814,24 +833,23 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
         if (t + kFWaves < nt) p0 = step(t + kFWaves, other, p1, mine);
       }
     } else {
-      // a lane: two quarter rows of K and two of V, in rows l / 4 and 16 + l / 4
+      // bank tiles one at a time: the other waves of the CU cover their latency
+      int t = tb + wave;
+      for (; t < min(nt, pl.nb); t += kFWaves) {
+        issue_bank(t, mine);
+        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+        asm volatile("" ::: "memory");
+        compute(true, t, mine, mine + TB, ~0ull);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        asm volatile("" ::: "memory");
+      }
+      // quantised rows through registers, one tile ahead; a lane: two quarter rows of K and two
+      // of V, in rows l / 4 and 16 + l / 4
       Quarter<FMT, D> xk[2], xv[2];
       const int part4 = l & 3;
       uint64_t pcur = 0, pnext = 0;
-      bool bnext = false;
-      auto fetch = [&](int t) {
+      auto fetch = [&](int t) __attribute__((always_inline)) {
         if (t >= nt) return;
-        bnext = t < pl.nb;
-        if (bnext) {
-#pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const int slot = t * kFK + 16 * g + (l >> 2);
-            xk[g].load_bank(reinterpret_cast<const uint16_t *>(bk) + (size_t)slot * D, part4, slot < pl.m);
-            xv[g].load_bank(reinterpret_cast<const uint16_t *>(bv) + (size_t)slot * D, part4, slot < pl.m);
-          }
-          pnext = ~0ull;
-          return;
-        }
         const int pos = tile_pos(pl, kFK, t);
         pw.seek(pos >> c.lps);
 #pragma unroll
@@ -844,17 +862,17 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
         }
         pnext = present_keys<kFK>(pw, pos, c.lps);
       };
-      fetch(tb + wave);
-      for (int t = tb + wave; t < nt; t += kFWaves) {
+      fetch(t);
+      for (; t < nt; t += kFWaves) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          xk[g].template store<false>(mine, 16 * g + (l >> 2), part4, bnext);
-          xv[g].template store<true>(mine + TB, 16 * g + (l >> 2), part4, bnext);
+          xk[g].template store<false>(mine, 16 * g + (l >> 2), part4);
+          xv[g].template store<true>(mine + TB, 16 * g + (l >> 2), part4);
         }
         pcur = pnext;
         fetch(t + kFWaves);
         __builtin_amdgcn_wave_barrier();  // one wave: its LDS operations run in order
-        compute(t, mine, mine + TB, pcur);
+        compute(false, t, mine, mine + TB, pcur);
         __builtin_amdgcn_wave_barrier();
       }
     }
@@ -873,6 +891,16 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
       const int pos = tile_pos(pl, kFK, t);
       const bool kok = (okbits >> n) & 1;
       const size_t krow = row_of(n);
+      // the values are on their way while the scores are computed
+      float vx[D / 32][16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
+        const bool ok = (okbits >> k) & 1;
+        const size_t vrow = row_of(k);
+#pragma unroll
+        for (int t2 = 0; t2 < D / 32; ++t2) vx[t2][i] = ok ? load_f32<F, D>(vp, vs, vrow, 32 * t2 + n) : 0.0f;
+      }
       f32x16 sc = {};
 #pragma unroll
       for (int k = 0; k < KC; ++k) {
@@ -908,29 +936,24 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_few(Pages c, Mas
       rows.lrun = __builtin_fmaf(rows.lrun, corr, ps);
 #pragma unroll
       for (int t2 = 0; t2 < D / 32; ++t2) {
-        float vx[16];
         bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
-          vx[i] = (okbits >> k) & 1 ? load_f32<F, D>(vp, vs, row_of(k), 32 * t2 + n) : 0.0f;
-          bad |= (__float_as_uint(vx[i]) & 0x7f800000u) == 0x7f800000u;
-        }
+        for (int i = 0; i < 16; ++i) bad |= (__float_as_uint(vx[t2][i]) & 0x7f800000u) == 0x7f800000u;
         rows.o[t2] *= corr;
         if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it
           f32x16 kinds = {};
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const uint32_t u = __float_as_uint(vx[i]);
+            const uint32_t u = __float_as_uint(vx[t2][i]);
             const float kind = (u & 0x7fffffffu) < 0x7f800000u ? 0.0f : ((u & 0x7fffffffu) > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
             kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> i) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
-            if (kind != 0.0f) vx[i] = 0.0f;
+            if (kind != 0.0f) vx[t2][i] = 0.0f;
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[i], pw_[i], rows.o[t2], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[t2][i], pw_[i], rows.o[t2], 0, 0, 0);
       }
     };
     for (int t = tb + wave; t < nt; t += kFWaves) {
