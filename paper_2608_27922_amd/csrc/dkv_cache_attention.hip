@@ -98,12 +98,14 @@ struct PageWindow {
 };
 
 // Physical 16-byte chunk of logical chunk c of row r (K: conflict-free 16-byte reads of
-// one chunk across 16 rows; V: conflict-free transposed 8-byte reads of 4 chunks across
-// 4 rows).
+// one chunk across 16 rows; V: conflict-free transposed 8-byte reads of 4 chunks across 4
+// rows, or of 2 chunks across 8 rows).
 template <int D>
 __device__ __forceinline__ int k_swz(int r, int c) { return c ^ (r % (D / 8)); }
 template <int D>
-__device__ __forceinline__ int v_swz(int r, int c) { return c ^ ((4 * (r % 4)) % (D / 8)); }
+__device__ __forceinline__ int v_swz(int r, int c) {
+  return c ^ (D == 128 ? 4 * (r % 4) : 4 * ((r >> 1) % 2)) ^ (2 * ((r >> 2) % 2));
+}
 
 // Direct-to-LDS loads of 8 rows (2 D bytes each, `valid` of them, the others as zeros)
 // of K and V into rows r0 .. r0 + 7 of a tile.  Lane i of a 1 KB load fetches the
@@ -127,7 +129,7 @@ __device__ __forceinline__ Rows8<D> rows8_offsets() {
   }
   return o;
 }
-// K's swizzle depends on the row modulo D / 8, V's modulo 4.
+// K's swizzle depends on the row modulo D / 8, V's modulo 8.
 template <int D>
 __device__ __forceinline__ void rows8_issue(int rsub, int pc, const int *voff, const unsigned char *kp,
                                             const unsigned char *vp, int valid, int r0, char *kt, char *vt) {
@@ -191,6 +193,18 @@ struct Quarter {
 constexpr int waitcnt_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
 __device__ __forceinline__ void stage_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
+// Whether this lane or the row's other lane says so (every lane takes part in the exchange).
+__device__ __forceinline__ bool either_half(bool x) {
+  const int y = __shfl_xor((int)x, 32, 64);
+  return x | (y != 0);
+}
+
+// Weight sum of a row: NaN-marked (-1) where its keys' scores were all -inf.
+__device__ __forceinline__ float row_sum(float mx, float l, bool keys) {
+  return keys && mx == -INFINITY && l == 0.0f ? -1.0f : l;
+}
+__device__ __forceinline__ float inv_sum(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : NAN); }
+
 // What one wave (32 rows, row n = lane % 32, half h = lane / 32) keeps while it walks keys.
 template <int D>
 struct Rows {
@@ -201,6 +215,18 @@ struct Rows {
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
     mrun = -INFINITY, lrun = 0.0f, any = false;
+  }
+  // (maximum, sum) of the row, and the outputs: put(chunk of 4 elements, values)
+  __device__ __forceinline__ float2 stats() const {
+    return float2{mrun, row_sum(mrun, lrun + __shfl_xor(lrun, 32, 64), either_half(any))};
+  }
+  template <class F>
+  __device__ __forceinline__ void outputs(F put) const {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) put(8 * t + 2 * g + h, float4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]});
   }
 };
 
@@ -258,12 +284,6 @@ __device__ __forceinline__ u32x4 v_operand(const char *vt, int sub, int kst, int
       (lds_i16x4 *)(vt + kb * (2 * D) + 16 * v_swz<D>(kb, dvb >> 1) + 8 * (dvb & 1)));
   const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
   return u32x4{a[0], a[1], b[0], b[1]};
-}
-
-// Whether this lane or the row's other lane says so (every lane takes part in the exchange).
-__device__ __forceinline__ bool either_half(bool x) {
-  const int y = __shfl_xor((int)x, 32, 64);
-  return x | (y != 0);
 }
 
 // Softmax update of one tile of one wave from its scores (masked ones are -inf); pb: the
@@ -340,6 +360,35 @@ __device__ __forceinline__ void product(Rows<D> &r, const uint32_t (*pb)[8], con
   }
 }
 
+// Whether a tile of BYTES in LDS holds a NaN or an infinity (bf16; asked by whole waves).
+template <int BYTES>
+__device__ __forceinline__ bool has_nonfinite(const char *vt) {
+  const int l = threadIdx.x & 63;
+  uint32_t bad = 0;
+#pragma unroll 4
+  for (int j = 0; j < BYTES / 1024; ++j) {
+    const u32x4 x = *reinterpret_cast<const u32x4 *>(vt + j * 1024 + 16 * l);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)  // an exponent of all ones plus one carries into its half's sign bit
+      bad |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+  }
+  return __any(bad != 0);
+}
+// Such values become zeros, by NT threads.
+template <int BYTES, int NT>
+__device__ __forceinline__ void zero_nonfinite(char *vt) {
+  for (int j = threadIdx.x % NT; j < BYTES / 16; j += NT) {
+    u32x4 x = *reinterpret_cast<const u32x4 *>(vt + 16 * j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+      if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
+    }
+    *reinterpret_cast<u32x4 *>(vt + 16 * j) = x;
+  }
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+}
+
 // In a tile that some rows see in part, a NaN or an infinity of V would reach the others
 // through 0 x inf.  Such values are added to the rows that see them (vis: bit k of a lane
 // for key k + 4 h of its row), as sums of the kinds that a row sees, and become zeros in
@@ -347,16 +396,7 @@ __device__ __forceinline__ void product(Rows<D> &r, const uint32_t (*pb)[8], con
 template <int D, int NSUB, int NT>
 __device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool work) {
   constexpr int kBytes = NSUB * 32 * 2 * D;
-  const int l = threadIdx.x & 63;
-  uint32_t bad = 0;
-#pragma unroll 4
-  for (int j = 0; j < kBytes / 1024; ++j) {
-    const u32x4 x = *reinterpret_cast<const u32x4 *>(vt + j * 1024 + 16 * l);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)  // an exponent of all ones plus one carries into its half's sign bit
-      bad |= ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-  }
-  if (!__any(bad != 0)) return;
+  if (!has_nonfinite<kBytes>(vt)) return;
   if (work) {
 #pragma unroll 1
     for (int t2 = 0; t2 < D / 32; ++t2) {
@@ -387,16 +427,7 @@ __device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool w
     __builtin_amdgcn_s_waitcnt(0xc07f);
     stage_barrier();  // every wave has read the tile
   }
-  for (int j = (NT > 64 ? (int)threadIdx.x : l); j < kBytes / 16; j += NT) {
-    u32x4 x = *reinterpret_cast<const u32x4 *>(vt + 16 * j);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
-      if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
-    }
-    *reinterpret_cast<u32x4 *>(vt + 16 * j) = x;
-  }
-  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  zero_nonfinite<kBytes, NT>(vt);
   if constexpr (NT > 64) stage_barrier();
 }
 
@@ -415,12 +446,12 @@ struct WaveMask {
 // Bits below x of 64.
 __device__ __forceinline__ uint64_t bits_below(int x) { return x <= 0 ? 0 : (x >= 64 ? ~0ull : (1ull << x) - 1); }
 
-// Keys of the tile at pos that this lane's row sees, bit k for key k + 4 h (so that the bits
-// of the lane's score registers are at 8 (i / 4) + i % 4); present: the tile's keys in pages
-// that are there.
-__device__ __forceinline__ uint64_t visible_bits(const WaveMask &w, int pos, uint64_t present) {
+// Keys of the tile at pos that this lane's row sees, bit k for key k + 4 g (so that the bits
+// of the lane's score registers are in the same places for every lane group g); present: the
+// tile's keys in pages that are there.
+__device__ __forceinline__ uint64_t visible_bits(const WaveMask &w, int pos, uint64_t present, int g) {
   const uint64_t m = bits_below(w.row.hi - pos) & (~bits_below(w.row.lo - pos) | bits_below(w.sink - pos)) & present;
-  return m >> (4 * ((threadIdx.x & 63) >> 5));
+  return m >> (4 * g);
 }
 template <int NSUB>
 __device__ __forceinline__ bool mask_cache(f32x16 *sc, uint64_t vis) {
@@ -452,12 +483,6 @@ __device__ __forceinline__ uint64_t present_keys(const PageWindow &pw, int pos, 
     if (pw.page(c0 + j) >= 0) bits |= ((1ull << (1 << lps)) - 1) << (j << lps);
   return KT == 64 ? bits : (bits | ~0xffffffffull);
 }
-
-// Weight sum of a row: NaN-marked (-1) where its keys' scores were all -inf.
-__device__ __forceinline__ float row_sum(float mx, float l, bool keys) {
-  return keys && mx == -INFINITY && l == 0.0f ? -1.0f : l;
-}
-__device__ __forceinline__ float inv_sum(float l) { return l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : NAN); }
 
 // Row r (token, head of the group) of a row block -> its packed row and query head.
 struct RowAt {
@@ -550,7 +575,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       } else if (whole) {
         rows.any = true;
       } else {
-        vis = visible_bits(wm, pos, present);
+        vis = visible_bits(wm, pos, present, lh);
         rows.any |= mask_cache<2>(sc, vis);
       }
       softmax_update<D, 2>(rows, sc, pb, qs.scale_log2);
@@ -658,37 +683,420 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     }
   }
   if (!work) return;
-  const bool any = either_half(rows.any);
-  const float ltot = row_sum(rows.mrun, rows.lrun + __shfl_xor(rows.lrun, 32, 64), any);
+  const float2 ml = rows.stats();
   if (!rv) return;
   if (part.ml) {
     const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
     const size_t row = (size_t)split * nrow + ((size_t)s * c.max_new + at.i) * qs.nh + at.hq;
-    if (lh == 0) part.ml[row] = float2{rows.mrun, ltot};
-#pragma unroll
-    for (int t2 = 0; t2 < D / 32; ++t2)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4 *>(part.o + row * D + 32 * t2 + 8 * g + 4 * lh) =
-            float4{rows.o[t2][4 * g], rows.o[t2][4 * g + 1], rows.o[t2][4 * g + 2], rows.o[t2][4 * g + 3]};
+    if (lh == 0) part.ml[row] = ml;
+    rows.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(part.o + row * D + 4 * chunk) = x; });
     return;
   }
-  const float inv = inv_sum(ltot);
+  const float inv = inv_sum(ml.y);
   uint16_t *out = static_cast<uint16_t *>(qs.out) + at.t * qs.ot + (size_t)at.hq * qs.oh;
-#pragma unroll
-  for (int t2 = 0; t2 < D / 32; ++t2)
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<u32x2 *>(out + 32 * t2 + 8 * g + 4 * lh) =
-          u32x2{pack_bf16x2(rows.o[t2][4 * g] * inv, rows.o[t2][4 * g + 1] * inv),
-                pack_bf16x2(rows.o[t2][4 * g + 2] * inv, rows.o[t2][4 * g + 3] * inv)};
+  rows.outputs([&](int chunk, float4 x) {
+    *reinterpret_cast<u32x2 *>(out + 4 * chunk) = u32x2{pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv)};
+  });
 }
+
+// ---------------------------------------------------------------------------
+// Few rows (bf16), 16 per wave: the same steps on v_mfma_f32_16x16x32_bf16 over tiles of 32
+// keys.  Lane (g, n) = (l / 16, l % 16) holds row n; register i of score tile st is key
+// 16 st + 4 g + i, register i of output tile t is element 16 t + 4 g + i.  Half the registers
+// and matrix cycles of a 32-row tile, so that a CU holds enough waves to keep its loads coming.
+// ---------------------------------------------------------------------------
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+template <int D>
+struct Wave16 {
+  static constexpr int R = 16;
+  bf16x8 qf[D / 32];
+  f32x4 o[D / 16];
+  float mrun, lrun;
+  bool any;
+  __device__ __forceinline__ void init(const uint16_t *q, bool ok) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int kk = 0; kk < D / 32; ++kk) {
+      u32x4 x = {0, 0, 0, 0};
+      if (ok) x = *reinterpret_cast<const u32x4 *>(q + 32 * kk + 8 * g);
+      qf[kk] = __builtin_bit_cast(bf16x8, x);
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
+    mrun = -INFINITY, lrun = 0.0f, any = false;
+  }
+  static __device__ __forceinline__ u32x4 v_op(const char *vt, int t) {
+    const int l = threadIdx.x & 63, g = l >> 4, cq = l & 15;
+    const int ka = 4 * g + (cq >> 2), kb = ka + 16, dvb = 4 * t + (cq & 3);
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_i16x4 *)(vt + ka * (2 * D) + 16 * v_swz<D>(ka, dvb >> 1) + 8 * (dvb & 1)));
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_i16x4 *)(vt + kb * (2 * D) + 16 * v_swz<D>(kb, dvb >> 1) + 8 * (dvb & 1)));
+    const u32x2 a = __builtin_bit_cast(u32x2, lo), b = __builtin_bit_cast(u32x2, hi);
+    return u32x4{a[0], a[1], b[0], b[1]};
+  }
+  // One tile: nvalid keys (bank tiles), or the keys of vis where not `whole`.
+  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint64_t vis) {
+    const int l = threadIdx.x & 63, g = l >> 4, n = l & 15;
+    f32x4 sc[2];
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const int key = 16 * st + n;
+      f32x4 acc = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 32; ++kk)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(kt + key * (2 * D) + 16 * k_swz<D>(key, 4 * kk + g))),
+            qf[kk], acc, 0, 0, 0);
+      sc[st] = acc;
+    }
+    if (!whole) {
+      bool some = false;
+#pragma unroll
+      for (int st = 0; st < 2; ++st)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if ((uint32_t)vis & (1u << (16 * st + i))) some = true;
+          else sc[st][i] = -INFINITY;
+        }
+      any |= some;
+    } else {
+      any = true;
+      if (nvalid < 32) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (16 * st + 4 * g + i >= nvalid) sc[st][i] = -INFINITY;
+      }
+    }
+    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+    uint32_t pb[4];
+    float psum = 0.0f;
+    auto exps = [&](float moff) {
+      psum = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1)], c, moff));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1) + 1], c, moff));
+        pb[e] = pack_bf16x2(p0, p1);
+        psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[e]), ones, psum, false);
+      }
+    };
+    exps(-mrun * c);
+    const bool over = !(psum <= kLazyLimit);
+    if (__any(over)) {  // as softmax_update
+      int raise = over;
+      raise |= __shfl_xor(raise, 16, 64);
+      raise |= __shfl_xor(raise, 32, 64);
+      float tmax = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                         fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, 64));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+      const float mnew = raise ? fmaxf(mrun, tmax) : mrun;
+      const float mref = mnew == -INFINITY ? 0.0f : mnew;
+      const float corr = raise ? __builtin_amdgcn_exp2f((mrun - mref) * c) : 1.0f;
+      mrun = mnew;
+      lrun *= corr;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) o[t] *= corr;
+      exps(-mref * c);
+    }
+    lrun += psum;
+    if (!whole) purge(vt, vis);
+    const u32x4 bp = {pb[0], pb[1], pb[2], pb[3]};
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v_op(vt, t)), __builtin_bit_cast(bf16x8, bp),
+                                                     o[t], 0, 0, 0);
+  }
+  // As the function of that name for 32 rows.
+  __device__ __forceinline__ void purge(char *vt, uint64_t vis) {
+    if (!has_nonfinite<64 * D>(vt)) return;
+    u32x4 bv;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int k = 16 * (e >> 1) + 2 * (e & 1);
+      bv[e] = ((uint32_t)(vis >> k) & 1 ? 0x3f80u : 0u) | ((uint32_t)(vis >> (k + 1)) & 1 ? 0x3f800000u : 0u);
+    }
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      u32x4 a = v_op(vt, t);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) a[e] = kind_of(a[e] & 0xffffu) | (kind_of(a[e] >> 16) << 16);
+      f32x4 kinds = {};
+      kinds = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, bv), kinds, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[t][i] += value_of_kinds(kinds[i]);
+    }
+    zero_nonfinite<64 * D, 64>(vt);
+  }
+  // (maximum, sum) of the row, and the outputs as float4 chunks: put(chunk of 4 elements, values)
+  __device__ __forceinline__ float2 stats() const {
+    int a = any;
+    a |= __shfl_xor(a, 16, 64);
+    a |= __shfl_xor(a, 32, 64);
+    float l = lrun + __shfl_xor(lrun, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    return float2{mrun, row_sum(mrun, l, a != 0)};
+  }
+  template <class F>
+  __device__ __forceinline__ void outputs(F put) const {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) put(4 * t + g, float4{o[t][0], o[t][1], o[t][2], o[t][3]});
+  }
+};
+
+// 32 rows per wave, tiles of 32 keys.
+template <int D>
+struct Wave32 {
+  static constexpr int R = 32;
+  bf16x8 qf[D / 16];
+  Rows<D> r;
+  __device__ __forceinline__ void init(const uint16_t *q, bool ok) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      u32x4 x = {0, 0, 0, 0};
+      if (ok) x = *reinterpret_cast<const u32x4 *>(q + 16 * kk + 8 * h);
+      qf[kk] = __builtin_bit_cast(bf16x8, x);
+    }
+    r.init();
+  }
+  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint64_t vis) {
+    f32x16 sc[1];
+    uint32_t pb[1][8];
+    scores<D, 1>(kt, qf, sc);
+    if (whole) {
+      r.any = true;
+      if (nvalid < 32) mask_bank<1>(sc, nvalid);
+    } else {
+      r.any |= mask_cache<1>(sc, vis);
+    }
+    softmax_update<D, 1>(r, sc, pb, c);
+    if (!whole) purge<D, 1, 64>(r, vt, vis, true);
+    product<D, 1>(r, pb, vt);
+  }
+  __device__ __forceinline__ float2 stats() const { return r.stats(); }
+  template <class F>
+  __device__ __forceinline__ void outputs(F put) const { r.outputs(put); }
+};
 
 // ---------------------------------------------------------------------------
 // Few rows, and fp32: a workgroup of 4 waves owns 32 rows; each wave walks tiles of 32 keys of
 // its own (every fourth), and the four results are joined at the end.
 // ---------------------------------------------------------------------------
 constexpr int kFWaves = 4, kFK = 32, kFLeast = 4;
+
+// What a workgroup of 4 waves knows about its row block of R rows and its run of key tiles.
+template <int R>
+struct Block {
+  int s, h, b, split, len, here, r0, tb, nt;
+  NewRows nr;
+  Plan pl;
+  // False where it has nothing to do.  Workgroup L runs on XCD L % 8: the row blocks and splits of
+  // a (sequence, head) are ranked XCD by XCD.
+  __device__ __forceinline__ bool init(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, int nrb,
+                                       int nsplit) {
+    const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
+    const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
+    const int rb = p % nrb, bs = p / nrb;
+    b = bs / nsplit, split = bs % nsplit, s = b / c.H, h = b % c.H;
+    nr = new_rows(c, s);
+    r0 = rb * R;
+    here = min(R, min(nr.n, c.max_new) * qs.G - r0);
+    if (here <= 0) return false;
+    len = seq_length(c, s);
+    pl = plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G);
+    const int used = splits_used<kFLeast>(pl.total, nsplit);
+    if (split >= used) return false;
+    split_range(pl.total, used, split, tb, nt);
+    return true;
+  }
+  __device__ __forceinline__ WaveMask wave_mask(const Mask &mask, const CacheQueries &qs, int i) const {
+    return WaveMask{seen_by(mask, len, nr.n, r0 / qs.G), seen_by(mask, len, nr.n, (r0 + here - 1) / qs.G),
+                    seen_by(mask, len, nr.n, i), mask.sink};
+  }
+};
+
+// The four waves' results (in LDS, 128 D bytes apart: R rows of D floats, 16-byte chunk j of row r at j ^ (r % 8); wml: maxima and
+// sums) joined under their common maximum, and written out, or as partial results of a split call.  unit: the factor
+// of the maxima's unit to log2.
+template <int DT, int D, int R>
+__device__ __forceinline__ void join_waves(const char *lds, const float2 (*wml)[R], const Block<R> &k, const Pages &c,
+                                           const CacheQueries &qs, const Part &part, float unit) {
+  for (int e = threadIdx.x; e < k.here * (D / 4); e += 64 * kFWaves) {
+    const int rr = e / (D / 4), j = 4 * (e % (D / 4));
+    float M = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kFWaves; ++w) M = fmaxf(M, wml[w][rr].x);
+    float lt = 0.0f, a[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kFWaves; ++w) {
+      const float2 ml = wml[w][rr];
+      const float f = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
+      const float4 x = *reinterpret_cast<const float4 *>(lds + 4 * (w * 32 * D + rr * D + (j ^ (4 * (rr % 8)))));
+      lt = __builtin_fmaf(ml.y, f, lt);
+      a[0] = __builtin_fmaf(x.x, f, a[0]);
+      a[1] = __builtin_fmaf(x.y, f, a[1]);
+      a[2] = __builtin_fmaf(x.z, f, a[2]);
+      a[3] = __builtin_fmaf(x.w, f, a[3]);
+    }
+    const RowAt ra = row_at(k.nr, qs, k.h, k.r0 + rr);
+    if (part.ml) {
+      const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
+      const size_t row = (size_t)k.split * nrow + ((size_t)k.s * c.max_new + ra.i) * qs.nh + ra.hq;
+      if (j == 0) part.ml[row] = float2{M, lt};
+      *reinterpret_cast<float4 *>(part.o + row * D + j) = float4{a[0], a[1], a[2], a[3]};
+      continue;
+    }
+    const float inv = inv_sum(lt);
+    const size_t o = ra.t * qs.ot + (size_t)ra.hq * qs.oh + j;
+    if constexpr (DT == DKV_BF16)
+      *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(qs.out) + o) =
+          u32x2{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
+    else
+      *reinterpret_cast<float4 *>(static_cast<float *>(qs.out) + o) = float4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+  }
+}
+
+// R rows per workgroup: 16 or 32.
+template <int FMT, int D, int R>
+__global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1 : 2) void k_cache_attn_few(
+    Pages c, Mask mask, BankRows bank, CacheQueries qs, int nrb, int nsplit, Part part) {
+  constexpr bool FULL = FMT == DKV_CACHE_FULL;
+  constexpr int TB = kFK * 2 * D;  // one tile of K or V
+  // Stages of (K tile, V tile) per wave; the first holds the waves' results at the end.  Two arrays, so that
+  // reads of one are known not to wait for loads into the other.
+  __shared__ __attribute__((aligned(1024))) char st0[kFWaves * 2 * TB], st1[FULL ? kFWaves * 2 * TB : 16];
+  __shared__ float2 wml[kFWaves][R];
+  Block<R> k;
+  if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l % R;
+  const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
+  const WaveMask wm = k.wave_mask(mask, qs, at.i);
+  PageWindow pw;
+  pw.init(c, k.s);
+  const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)k.b * bank.cap * (2 * D);
+  const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)k.b * bank.cap * (2 * D);
+  char *mine = st0 + wave * 2 * TB, *other = st1 + (FULL ? wave * 2 * TB : 0);
+  std::conditional_t<R == 16, Wave16<D>, Wave32<D>> w;
+  w.init(static_cast<const uint16_t *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh, n < k.here);
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
+    const int pos = tile_pos(k.pl, kFK, t);
+    const bool whole = isbank || (present == ~0ull && wm.all(pos, kFK));
+    w.step(kt, vt, qs.scale_log2, isbank ? k.pl.m - t * kFK : kFK, whole, whole ? 0 : visible_bits(wm, pos, present, l / R));
+  };
+  const Rows8<D> ld = rows8_offsets<D>();
+  auto issue_bank = [&](int t, char *buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int r8 = t * kFK + 8 * g;
+      rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(k.pl.m - r8, 0, 8),
+                     8 * g, buf, buf + TB);
+    }
+  };
+  if constexpr (FULL) {
+    // two stages: a tile in flight while the other is used
+    auto issue = [&](int t, char *buf) -> uint64_t {
+      if (t >= k.nt) return 0;
+      if (t < k.pl.nb) {
+        issue_bank(t, buf);
+        return ~0ull;
+      }
+      const int pos = tile_pos(k.pl, kFK, t);
+      pw.seek(pos >> c.lps);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
+        int nv = bound(k.pl.hi - p8, 0, 8);
+        if (page < 0 || (p8 + 8 <= k.pl.lo && p8 >= mask.sink)) nv = 0;
+        const size_t row = pool_row(c, page < 0 ? 0 : page, k.h, p8);
+        rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * g, buf, buf + TB);
+      }
+      return present_keys<kFK>(pw, pos, c.lps);
+    };
+    constexpr int kTileLoads = 4 * 2 * Rows8<D>::kLoads;
+    auto step = [&](int t, char *buf, uint64_t present, char *next) __attribute__((always_inline)) {
+      const uint64_t nx = issue(t + kFWaves, next);
+      // this tile's loads are done, the next one's may be on their way
+      if (t + kFWaves < k.nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
+      else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      asm volatile("" ::: "memory");
+      compute(t < k.pl.nb, t, buf, buf + TB, present);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
+      asm volatile("" ::: "memory");
+      return nx;
+    };
+    uint64_t p0 = issue(k.tb + wave, mine), p1 = 0;
+    for (int t = k.tb + wave; t < k.nt; t += 2 * kFWaves) {
+      p1 = step(t, mine, p0, other);
+      if (t + kFWaves < k.nt) p0 = step(t + kFWaves, other, p1, mine);
+    }
+  } else {
+    // bank tiles one at a time: the other waves of the CU cover their latency
+    int t = k.tb + wave;
+    for (; t < min(k.nt, k.pl.nb); t += kFWaves) {
+      issue_bank(t, mine);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      asm volatile("" ::: "memory");
+      compute(true, t, mine, mine + TB, ~0ull);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      asm volatile("" ::: "memory");
+    }
+    // quantised rows through registers, two tiles ahead; a lane: two quarter rows of K and two of
+    // V, in rows l / 4 and 16 + l / 4
+    struct {
+      Quarter<FMT, D> k[2], v[2];
+      uint64_t present;
+    } f[2];
+    const int part4 = l & 3, lr = l >> 2;
+    auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
+      if (t >= k.nt) return;
+      const int pos = tile_pos(k.pl, kFK, t);
+      pw.seek(pos >> c.lps);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int p16 = pos + 16 * g, page = pw.page(p16 >> c.lps);
+        const bool ok = page >= 0 && p16 + lr < k.pl.hi && (p16 + 16 > k.pl.lo || p16 < mask.sink);
+        const size_t row = pool_row(c, page < 0 ? 0 : page, k.h, p16 + lr);
+        y.k[g].load(c.k, c.ks, row, part4, ok);
+        y.v[g].load(c.v, c.vs, row, part4, ok);
+      }
+      y.present = present_keys<kFK>(pw, pos, c.lps);
+    };
+    auto step = [&](auto &y, int t) __attribute__((always_inline)) {
+      // the reads of the tile before are done: a wave's LDS operations run in order
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        y.k[g].template store<false>(mine, 16 * g + lr, part4);
+        y.v[g].template store<true>(mine + TB, 16 * g + lr, part4);
+      }
+      const uint64_t present = y.present;
+      fetch(y, t + 2 * kFWaves);
+      __builtin_amdgcn_wave_barrier();
+      compute(false, t, mine, mine + TB, present);
+      __builtin_amdgcn_wave_barrier();
+    };
+    fetch(f[0], t);
+    fetch(f[1], t + kFWaves);
+    for (; t < k.nt; t += 2 * kFWaves) {
+      step(f[0], t);
+      if (t + kFWaves < k.nt) step(f[1], t + kFWaves);
+    }
+  }
+
+  if (n < k.here) {
+    float *mo = reinterpret_cast<float *>(mine) + n * D;  // in the stages that only this wave uses
+    const float2 ml = w.stats();
+    if (l < R) wml[wave][n] = ml;
+    w.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(mo + 4 * (chunk ^ (n % 8))) = x; });
+  }
+  __syncthreads();
+  join_waves<DKV_BF16, D, R>(st0, wml, k, c, qs, part, qs.scale_log2);
+}
 
 // fp32 scores and products on v_mfma_f32_32x32x2_f32, keys and values straight from memory.
 // K step 4 c + j takes dims 8 c + j and 8 c + 4 + j of both operands.
@@ -723,335 +1131,161 @@ __device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8
   }
 }
 
-template <int DT, int FMT, int D>
-__global__ __launch_bounds__(64 * kFWaves, (DT == DKV_BF16 && FMT != DKV_CACHE_FULL) || D == 64 ? 2 : 1) void k_cache_attn_few(Pages c, Mask mask, BankRows bank, CacheQueries qs,
+template <int FMT, int D>
+__global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mask mask, BankRows bank, CacheQueries qs,
                                                                    int nrb, int nsplit, Part part) {
-  constexpr bool BF = DT == DKV_BF16, FULL = FMT == DKV_CACHE_FULL;
-  constexpr int TB = kFK * 2 * D;  // one bf16 tile of K or V
-  // Stages of (K tile, V tile) per wave; the first holds the waves' results at the end (32 rows of D floats).
-  // Two arrays, so that reads of one are known not to wait for loads into the other.
-  __shared__ __attribute__((aligned(1024))) char st0[kFWaves * 2 * TB], st1[BF && FULL ? kFWaves * 2 * TB : 16];
+  __shared__ __attribute__((aligned(16))) char st0[kFWaves * 32 * D * 4];  // the waves' results at the end
   __shared__ float2 wml[kFWaves][32];
-  const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
-  const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
-  const int rb = p % nrb, bs = p / nrb, b = bs / nsplit, split = bs % nsplit;
-  const int s = b / c.H, h = b % c.H;
-  const NewRows nr = new_rows(c, s);
-  const int nrows = min(nr.n, c.max_new) * qs.G, r0 = rb * 32;
-  if (r0 >= nrows) return;
-  const int len = seq_length(c, s);
-  const int here = min(32, nrows - r0);
+  Block<32> k;
+  if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
-  const RowAt at = row_at(nr, qs, h, r0 + min(n, here - 1));
-  WaveMask wm;
-  wm.sink = mask.sink;
-  wm.row = seen_by(mask, len, nr.n, at.i);
-  wm.first = seen_by(mask, len, nr.n, r0 / qs.G);
-  wm.last = seen_by(mask, len, nr.n, (r0 + here - 1) / qs.G);
-  const Plan pl = plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G);
-  const int used = splits_used<kFLeast>(pl.total, nsplit);
-  if (split >= used) return;
-  int tb, nt;
-  split_range(pl.total, used, split, tb, nt);
+  const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
+  const WaveMask wm = k.wave_mask(mask, qs, at.i);
   PageWindow pw;
-  pw.init(c, s);
+  pw.init(c, k.s);
   Rows<D> rows;
   rows.init();
-  constexpr int EB = BF ? 2 : 4;  // bytes of a bank element
-  const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (EB * D);
-  const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (EB * D);
-  char *mine = st0 + wave * 2 * TB, *other = st1 + (BF && FULL ? wave * 2 * TB : 0);
-  if constexpr (BF) {
-    bf16x8 qf[D / 16];
-    load_q<D>(qf, qs, at, n < here);
-    auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
-      const int pos = tile_pos(pl, kFK, t);
-      f32x16 sc[1];
-      uint32_t pb[1][8];
-      scores<D, 1>(kt, qf, sc);
-      uint64_t vis = 0;
-      bool whole = true;
-      if (isbank) {
-        const int nv = pl.m - t * kFK;
-        if (nv < kFK) mask_bank<1>(sc, nv);
-        rows.any = true;
-      } else if (present == ~0ull && wm.all(pos, kFK)) {
-        rows.any = true;
-      } else {
-        whole = false;
-        vis = visible_bits(wm, pos, present);
-        rows.any |= mask_cache<1>(sc, vis);
-      }
-      softmax_update<D, 1>(rows, sc, pb, qs.scale_log2);
-      if (!whole) purge<D, 1, 64>(rows, vt, vis, true);
-      product<D, 1>(rows, pb, vt);
-    };
-    const Rows8<D> ld = rows8_offsets<D>();
-    auto issue_bank = [&](int t, char *buf) __attribute__((always_inline)) {
+  const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)k.b * bank.cap * (4 * D);
+  const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)k.b * bank.cap * (4 * D);
+  constexpr int KC = D / 8;
+  float4 qf[KC];
+  {
+    const float *q = static_cast<const float *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int r8 = t * kFK + 8 * g;
-        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8),
-                       8 * g, buf, buf + TB);
-      }
-    };
-    if constexpr (FULL) {
-      // two stages: a tile in flight while the other is used
-      auto issue = [&](int t, char *buf) -> uint64_t {
-        if (t >= nt) return 0;
-        if (t < pl.nb) {
-          issue_bank(t, buf);
-          return ~0ull;
-        }
-        const int pos = tile_pos(pl, kFK, t);
-        pw.seek(pos >> c.lps);
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
-          int nv = bound(pl.hi - p8, 0, 8);
-          if (page < 0 || (p8 + 8 <= pl.lo && p8 >= mask.sink)) nv = 0;
-          const size_t row = pool_row(c, page < 0 ? 0 : page, h, p8);
-          rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * g, buf, buf + TB);
-        }
-        return present_keys<kFK>(pw, pos, c.lps);
-      };
-      constexpr int kTileLoads = 4 * 2 * Rows8<D>::kLoads;
-      auto step = [&](int t, char *buf, uint64_t present, char *next) __attribute__((always_inline)) {
-        const uint64_t nx = issue(t + kFWaves, next);
-        // this tile's loads are done, the next one's may be on their way
-        if (t + kFWaves < nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
-        else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-        asm volatile("" ::: "memory");
-        compute(t < pl.nb, t, buf, buf + TB, present);
-        __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
-        asm volatile("" ::: "memory");
-        return nx;
-      };
-      uint64_t p0 = issue(tb + wave, mine), p1 = 0;
-      for (int t = tb + wave; t < nt; t += 2 * kFWaves) {
-        p1 = step(t, mine, p0, other);
-        if (t + kFWaves < nt) p0 = step(t + kFWaves, other, p1, mine);
-      }
-    } else {
-      // bank tiles one at a time: the other waves of the CU cover their latency
-      int t = tb + wave;
-      for (; t < min(nt, pl.nb); t += kFWaves) {
-        issue_bank(t, mine);
-        __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-        asm volatile("" ::: "memory");
-        compute(true, t, mine, mine + TB, ~0ull);
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        asm volatile("" ::: "memory");
-      }
-      // quantised rows through registers, one tile ahead; a lane: two quarter rows of K and two
-      // of V, in rows l / 4 and 16 + l / 4
-      Quarter<FMT, D> xk[2], xv[2];
-      const int part4 = l & 3;
-      uint64_t pcur = 0, pnext = 0;
-      auto fetch = [&](int t) __attribute__((always_inline)) {
-        if (t >= nt) return;
-        const int pos = tile_pos(pl, kFK, t);
-        pw.seek(pos >> c.lps);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const int p16 = pos + 16 * g, at_pos = p16 + (l >> 2), page = pw.page(p16 >> c.lps);
-          const bool ok = page >= 0 && at_pos < pl.hi && (p16 + 16 > pl.lo || p16 < mask.sink);
-          const size_t row = pool_row(c, page < 0 ? 0 : page, h, at_pos);
-          xk[g].load(c.k, c.ks, row, part4, ok);
-          xv[g].load(c.v, c.vs, row, part4, ok);
-        }
-        pnext = present_keys<kFK>(pw, pos, c.lps);
-      };
-      fetch(t);
-      for (; t < nt; t += kFWaves) {
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          xk[g].template store<false>(mine, 16 * g + (l >> 2), part4);
-          xv[g].template store<true>(mine + TB, 16 * g + (l >> 2), part4);
-        }
-        pcur = pnext;
-        fetch(t + kFWaves);
-        __builtin_amdgcn_wave_barrier();  // one wave: its LDS operations run in order
-        compute(false, t, mine, mine + TB, pcur);
-        __builtin_amdgcn_wave_barrier();
-      }
-    }
-  } else {
-    constexpr int KC = D / 8;
-    float4 qf[KC];
-    {
-      const float *q = static_cast<const float *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh;
-#pragma unroll
-      for (int k = 0; k < KC; ++k) qf[k] = *reinterpret_cast<const float4 *>(q + 8 * k + 4 * lh);
-    }
-    auto tile = [&](auto fmt, int t, const unsigned char *kp, const uint8_t *ks, const unsigned char *vp, const uint8_t *vs,
-                    auto row_of, uint32_t okbits) __attribute__((always_inline)) {
-      // okbits: rows of the tile that may be read; the others count as zeros
-      constexpr int F = decltype(fmt)::value;
-      const int pos = tile_pos(pl, kFK, t);
-      const bool kok = (okbits >> n) & 1;
-      const size_t krow = row_of(n);
-      // the values are on their way while the scores are computed
-      float vx[D / 32][16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
-        const bool ok = (okbits >> k) & 1;
-        const size_t vrow = row_of(k);
-#pragma unroll
-        for (int t2 = 0; t2 < D / 32; ++t2) vx[t2][i] = ok ? load_f32<F, D>(vp, vs, vrow, 32 * t2 + n) : 0.0f;
-      }
-      f32x16 sc = {};
-#pragma unroll
-      for (int k = 0; k < KC; ++k) {
-        float4 kx = {0, 0, 0, 0};
-        if (kok) kx = load_f32x4<F, D>(kp, ks, krow, 8 * k + 4 * lh);
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.x, qf[k].x, sc, 0, 0, 0);
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.y, qf[k].y, sc, 0, 0, 0);
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.z, qf[k].z, sc, 0, 0, 0);
-        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.w, qf[k].w, sc, 0, 0, 0);
-      }
-      uint32_t vis = 0;
-      float tmax = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int k = 8 * (i >> 2) + 4 * lh + (i & 3);
-        const bool ok = ((okbits >> k) & 1) && (t < pl.nb || sees(wm.row, wm.sink, pos + k));
-        if (ok) vis |= 1u << i;
-        sc[i] = ok ? sc[i] * qs.scale_log2 : -INFINITY;
-        tmax = fmaxf(tmax, sc[i]);
-      }
-      rows.any |= vis != 0;
-      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
-      const float mnew = fmaxf(rows.mrun, tmax);
-      const float mref = mnew == -INFINITY ? 0.0f : mnew;
-      const float corr = exp2f(rows.mrun - mref);
-      rows.mrun = mnew;
-      float pw_[16], ps = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        pw_[i] = exp2f(sc[i] - mref);
-        ps += pw_[i];
-      }
-      rows.lrun = __builtin_fmaf(rows.lrun, corr, ps);
-#pragma unroll
-      for (int t2 = 0; t2 < D / 32; ++t2) {
-        bool bad = false;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) bad |= (__float_as_uint(vx[t2][i]) & 0x7f800000u) == 0x7f800000u;
-        rows.o[t2] *= corr;
-        if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it
-          f32x16 kinds = {};
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint32_t u = __float_as_uint(vx[t2][i]);
-            const float kind = (u & 0x7fffffffu) < 0x7f800000u ? 0.0f : ((u & 0x7fffffffu) > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
-            kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> i) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
-            if (kind != 0.0f) vx[t2][i] = 0.0f;
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[t2][i], pw_[i], rows.o[t2], 0, 0, 0);
-      }
-    };
-    for (int t = tb + wave; t < nt; t += kFWaves) {
-      if (t < pl.nb) {
-        const int nv = min(kFK, pl.m - t * kFK);
-        tile(std::integral_constant<int, DKV_CACHE_FULL>(), t, bk, nullptr, bv, nullptr,
-             [&](int k) { return (size_t)t * kFK + k; }, nv >= 32 ? 0xffffffffu : (1u << nv) - 1u);
-        continue;
-      }
-      const int pos = tile_pos(pl, kFK, t);
-      pw.seek(pos >> c.lps);
-      const int pa = pw.page(pos >> c.lps), pb = pw.page((pos + 16) >> c.lps);
-      uint32_t okbits = (pa >= 0 ? 0xffffu : 0u) | (pb >= 0 ? 0xffff0000u : 0u);
-      if (pl.hi - pos < 32) okbits &= (1u << (pl.hi - pos)) - 1u;
-      // rows before the window of every row block's token and behind the first tokens are not read
-      tile(std::integral_constant<int, FMT>(), t, c.k, c.ks, c.v, c.vs,
-           [&](int k) { return pool_row(c, max(k < 16 ? pa : pb, 0), h, pos + k); }, okbits);
-    }
+    for (int u = 0; u < KC; ++u) qf[u] = *reinterpret_cast<const float4 *>(q + 8 * u + 4 * lh);
   }
-
-  // the four waves' results, joined under their common maximum (bf16: of raw scores)
-  const float unit = BF ? qs.scale_log2 : 1.0f;
-  const bool any = either_half(rows.any);
-  const float lw = row_sum(rows.mrun, rows.lrun + __shfl_xor(rows.lrun, 32, 64), any);
-  float *mo = reinterpret_cast<float *>(mine);
-  if (n < here) {
-    if (lh == 0) wml[wave][n] = float2{rows.mrun, lw};
+  auto tile = [&](auto fmt, int t, const unsigned char *kp, const uint8_t *ks, const unsigned char *vp, const uint8_t *vs,
+                  auto row_of, uint32_t okbits) __attribute__((always_inline)) {
+    // okbits: rows of the tile that may be read; the others count as zeros
+    constexpr int F = decltype(fmt)::value;
+    const int pos = tile_pos(k.pl, kFK, t);
+    const bool kok = (okbits >> n) & 1;
+    const size_t krow = row_of(n);
+    // the values are on their way while the scores are computed
+    float vx[D / 32][16];
 #pragma unroll
-    for (int t2 = 0; t2 < D / 32; ++t2)
+    for (int i = 0; i < 16; ++i) {
+      const int key = 8 * (i >> 2) + 4 * lh + (i & 3);
+      const bool ok = (okbits >> key) & 1;
+      const size_t vrow = row_of(key);
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4 *>(mo + n * D + 4 * ((8 * t2 + 2 * g + lh) ^ (n % 8))) =
-            float4{rows.o[t2][4 * g], rows.o[t2][4 * g + 1], rows.o[t2][4 * g + 2], rows.o[t2][4 * g + 3]};
-  }
-  __syncthreads();
-  for (int e = threadIdx.x; e < here * (D / 4); e += 64 * kFWaves) {
-    const int rr = e / (D / 4), j = 4 * (e % (D / 4));
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kFWaves; ++w) M = fmaxf(M, wml[w][rr].x);
-    float lt = 0.0f, a[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int w = 0; w < kFWaves; ++w) {
-      const float2 ml = wml[w][rr];
-      const float f = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
-      const float4 x = *reinterpret_cast<const float4 *>(st0 + w * 2 * TB + 4 * (rr * D + (j ^ (4 * (rr % 8)))));
-      lt = __builtin_fmaf(ml.y, f, lt);
-      a[0] = __builtin_fmaf(x.x, f, a[0]);
-      a[1] = __builtin_fmaf(x.y, f, a[1]);
-      a[2] = __builtin_fmaf(x.z, f, a[2]);
-      a[3] = __builtin_fmaf(x.w, f, a[3]);
+      for (int t2 = 0; t2 < D / 32; ++t2) vx[t2][i] = ok ? load_f32<F, D>(vp, vs, vrow, 32 * t2 + n) : 0.0f;
     }
-    const RowAt ra = row_at(nr, qs, h, r0 + rr);
-    if (part.ml) {
-      const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
-      const size_t row = (size_t)split * nrow + ((size_t)s * c.max_new + ra.i) * qs.nh + ra.hq;
-      if (j == 0) part.ml[row] = float2{M, lt};
-      *reinterpret_cast<float4 *>(part.o + row * D + j) = float4{a[0], a[1], a[2], a[3]};
+    f32x16 sc = {};
+#pragma unroll
+    for (int u = 0; u < KC; ++u) {
+      float4 kx = {0, 0, 0, 0};
+      if (kok) kx = load_f32x4<F, D>(kp, ks, krow, 8 * u + 4 * lh);
+      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.x, qf[u].x, sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.y, qf[u].y, sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.z, qf[u].z, sc, 0, 0, 0);
+      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.w, qf[u].w, sc, 0, 0, 0);
+    }
+    uint32_t vis = 0;
+    float tmax = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = 8 * (i >> 2) + 4 * lh + (i & 3);
+      const bool ok = ((okbits >> key) & 1) && (t < k.pl.nb || sees(wm.row, wm.sink, pos + key));
+      if (ok) vis |= 1u << i;
+      sc[i] = ok ? sc[i] * qs.scale_log2 : -INFINITY;
+      tmax = fmaxf(tmax, sc[i]);
+    }
+    rows.any |= vis != 0;
+    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
+    const float mnew = fmaxf(rows.mrun, tmax);
+    const float mref = mnew == -INFINITY ? 0.0f : mnew;
+    const float corr = exp2f(rows.mrun - mref);
+    rows.mrun = mnew;
+    float pw_[16], ps = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      pw_[i] = exp2f(sc[i] - mref);
+      ps += pw_[i];
+    }
+    rows.lrun = __builtin_fmaf(rows.lrun, corr, ps);
+#pragma unroll
+    for (int t2 = 0; t2 < D / 32; ++t2) {
+      bool bad = false;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad |= (__float_as_uint(vx[t2][i]) & 0x7f800000u) == 0x7f800000u;
+      rows.o[t2] *= corr;
+      if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it
+        f32x16 kinds = {};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t u = __float_as_uint(vx[t2][i]);
+          const float kind = (u & 0x7fffffffu) < 0x7f800000u ? 0.0f : ((u & 0x7fffffffu) > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
+          kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> i) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
+          if (kind != 0.0f) vx[t2][i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[t2][i], pw_[i], rows.o[t2], 0, 0, 0);
+    }
+  };
+  for (int t = k.tb + wave; t < k.nt; t += kFWaves) {
+    if (t < k.pl.nb) {
+      const int nv = min(kFK, k.pl.m - t * kFK);
+      tile(std::integral_constant<int, DKV_CACHE_FULL>(), t, bk, nullptr, bv, nullptr,
+           [&](int key) { return (size_t)t * kFK + key; }, nv >= 32 ? 0xffffffffu : (1u << nv) - 1u);
       continue;
     }
-    const float inv = inv_sum(lt);
-    const size_t o = ra.t * qs.ot + (size_t)ra.hq * qs.oh + j;
-    if constexpr (BF)
-      *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(qs.out) + o) =
-          u32x2{pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv)};
-    else
-      *reinterpret_cast<float4 *>(static_cast<float *>(qs.out) + o) = float4{a[0] * inv, a[1] * inv, a[2] * inv, a[3] * inv};
+    const int pos = tile_pos(k.pl, kFK, t);
+    pw.seek(pos >> c.lps);
+    const int pa = pw.page(pos >> c.lps), pb = pw.page((pos + 16) >> c.lps);
+    uint32_t okbits = (pa >= 0 ? 0xffffu : 0u) | (pb >= 0 ? 0xffff0000u : 0u);
+    if (k.pl.hi - pos < 32) okbits &= (1u << (k.pl.hi - pos)) - 1u;
+    // rows before the window of every row block's token and behind the first tokens are not read
+    tile(std::integral_constant<int, FMT>(), t, c.k, c.ks, c.v, c.vs,
+         [&](int key) { return pool_row(c, max(key < 16 ? pa : pb, 0), k.h, pos + key); }, okbits);
   }
+
+  if (n < k.here) {
+    float *mo = reinterpret_cast<float *>(st0) + wave * 32 * D + n * D;
+    const float2 ml = rows.stats();
+    if (lh == 0) wml[wave][n] = ml;
+    rows.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(mo + 4 * (chunk ^ (n % 8))) = x; });
+  }
+  __syncthreads();
+  join_waves<DKV_F32, D, 32>(st0, wml, k, c, qs, part, 1.0f);  // maxima in log2 units
 }
 
 // Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  D / 4 lanes
-// per row; RB rows per row block, KT keys per tile of the kernel that wrote them.
-template <int DT, int D, int RB, int KT, int LEAST>
+// per row and split; SG splits of a row at a time, joined in LDS.  RB rows per row block, KT keys per tile of the
+// kernel that wrote them.
+template <int DT, int D, int RB, int KT, int LEAST, int SG>
 __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit,
                                                        Part part) {
-  constexpr int LR = D / 4;
+  constexpr int LR = D / 4, NR = 256 / LR / SG;  // rows per workgroup
   const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
-  const size_t row = (size_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
-  const int j = 4 * (threadIdx.x % LR);
-  if (row >= nrow) return;
+  const int lane = threadIdx.x % LR, sub = (threadIdx.x / LR) % SG, rr = threadIdx.x / LR / SG, j = 4 * lane;
+  const size_t row = (size_t)blockIdx.x * NR + rr;
   const unsigned per = (unsigned)c.max_new * qs.nh;  // < 2^31
-  const int s = (int)(row / per);
-  const unsigned rest = (unsigned)(row - (size_t)s * per);
-  const int i = (int)(rest / (unsigned)qs.nh), hq = (int)(rest % (unsigned)qs.nh), h = hq / qs.G;
-  const float2 ml0 = part.ml[row];  // read while the plan is on its way
-  const float4 x0 = *reinterpret_cast<const float4 *>(part.o + row * D + j);
-  const NewRows nr = new_rows(c, s);
-  const int n = min(nr.n, c.max_new);
-  if (i >= n) return;
-  const int r0 = (i * qs.G + hq - h * qs.G) / RB * RB, r1 = min(r0 + RB, n * qs.G) - 1;
-  const Plan pl = plan_of<KT>(mask, bank, s * c.H + h, seq_length(c, s), nr.n, r0 / qs.G, r1 / qs.G);
-  const int used = splits_used<LEAST>(pl.total, nsplit);
+  bool live = row < nrow;
+  int s = 0, i = 0, hq = 0, used = 0;
+  NewRows nr{0, 0};
+  if (live) {
+    s = (int)(row / per);
+    const unsigned rest = (unsigned)(row - (size_t)s * per);
+    i = (int)(rest / (unsigned)qs.nh), hq = (int)(rest % (unsigned)qs.nh);
+    nr = new_rows(c, s);
+    const int n = min(nr.n, c.max_new), h = hq / qs.G;
+    live = i < n;
+    if (live) {
+      const int r0 = (i * qs.G + hq - h * qs.G) / RB * RB, r1 = min(r0 + RB, n * qs.G) - 1;
+      const Plan pl = plan_of<KT>(mask, bank, s * c.H + h, seq_length(c, s), nr.n, r0 / qs.G, r1 / qs.G);
+      used = splits_used<LEAST>(pl.total, nsplit);
+    }
+  }
   const float unit = DT == DKV_BF16 ? qs.scale_log2 : 1.0f;  // the bf16 maxima are raw scores
-  float M = ml0.x;
-  for (int k = 1; k < used; ++k) M = fmaxf(M, part.ml[k * nrow + row].x);
-  const float w0 = ml0.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml0.x - M) * unit);
-  float l = ml0.y * w0, a[4] = {x0.x * w0, x0.y * w0, x0.z * w0, x0.w * w0};
-  for (int k = 1; k < used; ++k) {
+  float M = -INFINITY;
+  for (int k = 0; k < used; ++k) M = fmaxf(M, part.ml[k * nrow + row].x);
+  float l = 0.0f, a[4] = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = sub; k < used; k += SG) {
     const float2 ml = part.ml[k * nrow + row];
     const float4 x = *reinterpret_cast<const float4 *>(part.o + (k * nrow + row) * D + j);
     const float w = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
@@ -1061,6 +1295,21 @@ __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankR
     a[2] = __builtin_fmaf(x.z, w, a[2]);
     a[3] = __builtin_fmaf(x.w, w, a[3]);
   }
+  if constexpr (SG > 1) {
+    __shared__ float4 la[256];
+    __shared__ float ll[256];
+    la[threadIdx.x] = float4{a[0], a[1], a[2], a[3]};
+    ll[threadIdx.x] = l;
+    __syncthreads();
+    if (sub != 0) return;
+#pragma unroll
+    for (int k = 1; k < SG; ++k) {
+      const float4 x = la[threadIdx.x + k * LR];
+      l += ll[threadIdx.x + k * LR];
+      a[0] += x.x, a[1] += x.y, a[2] += x.z, a[3] += x.w;
+    }
+  }
+  if (!live) return;
   const float inv = inv_sum(l);
   const size_t o = (size_t)(nr.first + i) * qs.ot + (size_t)hq * qs.oh + j;
   if constexpr (DT == DKV_BF16)
@@ -1072,9 +1321,27 @@ __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankR
 
 constexpr int kCUs = 256;
 constexpr int kMaxSplit = 64;
-constexpr int kFewRows = 64;  // rows of a (sequence, kv head) up to which 32-row blocks are taken
+constexpr int kFewRows = 64;   // rows of a (sequence, kv head) up to which blocks of 16 or 32 rows are taken
+constexpr int kManySplits = 5; // splits from which a row's partial results are read 8 (16) at a time
 
-bool takes_few(const Pages &c, int dtype, int G) { return dtype != DKV_BF16 || (long long)c.max_new * G <= kFewRows; }
+// Rows per row block of a call: 16 or 32 with the keys over the waves, or 256.
+int block_rows(const Pages &c, int dtype, int G) {
+  const int64_t rows = (int64_t)c.max_new * G;
+  if (dtype != DKV_BF16) return 32;
+  return rows <= 16 ? 16 : (rows <= kFewRows ? 32 : kWRows);
+}
+
+template <int DT, int D, int RB, int KT, int LEAST>
+void combine(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, int nsplit, const Part &part,
+             hipStream_t s) {
+  constexpr int kGroups = 256 / (D / 4);
+  const int64_t nrow = (int64_t)c.S * c.max_new * qs.nh;  // < 2^31 (checked by the caller)
+  if (nsplit >= kManySplits)
+    k_cache_combine<DT, D, RB, KT, LEAST, kGroups><<<(unsigned)nrow, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
+  else
+    k_cache_combine<DT, D, RB, KT, LEAST, 1><<<(unsigned)((nrow + kGroups - 1) / kGroups), 256, 0, s>>>(c, mask, bank, qs,
+                                                                                                       nsplit, part);
+}
 
 template <int DT, int FMT, int D>
 hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, void *ws, int nsplit,
@@ -1086,20 +1353,25 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
     part.o = static_cast<float *>(ws);
     part.ml = reinterpret_cast<float2 *>(part.o + nrow * nsplit * D);
   }
-  const bool few = takes_few(c, DT, qs.G);
-  const int64_t nrb = ((int64_t)c.max_new * qs.G + (few ? 31 : kWRows - 1)) / (few ? 32 : kWRows);
+  const int R = block_rows(c, DT, qs.G);
+  const int64_t nrb = ((int64_t)c.max_new * qs.G + R - 1) / R;
   const int64_t grid = nrb * c.S * c.H * nsplit;
-  constexpr int kRows = 256 / (D / 4);
-  const int64_t cgrid = (nrow + kRows - 1) / kRows;
-  if (grid > 0x7fffffffLL || cgrid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
-  if (few) {
-    k_cache_attn_few<DT, FMT, D><<<(unsigned)grid, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
-    if (nsplit > 1)
-      k_cache_combine<DT, D, 32, kFK, kFLeast><<<(unsigned)cgrid, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
-  } else if constexpr (DT == DKV_BF16) {
-    k_cache_attn_wide<FMT, D><<<(unsigned)grid, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
-    if (nsplit > 1)
-      k_cache_combine<DT, D, kWRows, kWK, kWLeast><<<(unsigned)cgrid, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
+  if (grid > 0x7fffffffLL || nrow > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  const unsigned g = (unsigned)grid;
+  if constexpr (DT == DKV_BF16) {
+    if (R == kWRows) {
+      k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      if (nsplit > 1) combine<DT, D, kWRows, kWK, kWLeast>(c, mask, bank, qs, nsplit, part, s);
+    } else if (R == 32) {
+      k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
+    } else {
+      k_cache_attn_few<FMT, D, 16><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      if (nsplit > 1) combine<DT, D, 16, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
+    }
+  } else {
+    k_cache_attn_f32<FMT, D><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+    if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
   }
   return hipGetLastError();
 }
@@ -1114,8 +1386,9 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   const int G = nh / c.H;
   const int64_t nrow = (int64_t)c.S * c.max_new * nh;
   if (nrow == 0) return 1;
-  const bool few = takes_few(c, dtype, G);
-  const int KT = few ? kFK : kWK, RB = few ? 32 : kWRows, least = few ? kFLeast : kWLeast;
+  const int RB = block_rows(c, dtype, G);
+  const bool few = RB != kWRows;
+  const int KT = few ? kFK : kWK, least = few ? kFLeast : kWLeast;
   int64_t keys = (int64_t)c.cols << c.lps;
   if (mask.window > 0) {
     const int64_t seen = (int64_t)mask.window + (mask.causal ? c.max_new : 0) + mask.sink + KT;
@@ -1123,14 +1396,16 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   }
   const int64_t tiles = (keys + KT - 1) / KT + (bank.cap + KT - 1) / KT;
   const int64_t nwg = ((int64_t)c.max_new * G + RB - 1) / RB * c.S * c.H;
-  const int64_t slots = few && (dtype != DKV_BF16 || fmt != DKV_CACHE_FULL) ? 2 * kCUs : kCUs;
-  const double each = few ? kFWaves : 1;  // tiles walked at a time
+  const int64_t slots = few && (d == 64 || fmt != DKV_CACHE_FULL) && dtype == DKV_BF16 ? 2 * kCUs : kCUs;
+  // us per tile of a workgroup, and per workgroup
+  const double tile_us = dtype != DKV_BF16 ? (d == 64 ? 0.8 : 1.3) : (few ? (d == 64 ? 0.4 : 0.7) : (d == 64 ? 1.0 : 1.9));
+  const double start_us = few ? 5.0 : 8.0;
   int best = 1;
   double best_cost = 0.0;
   for (int S = 1; S <= kMaxSplit && (S == 1 || tiles / S >= least); ++S) {
     const double rounds = (double)((nwg * S + slots - 1) / slots);
-    double cost = rounds * ((double)((tiles + S - 1) / S) / each + 6);
-    if (S > 1) cost += 4.0 + (double)nrow * S * (8.0 * d + 16.0) / (4e12 * 1.6e-6);
+    double cost = rounds * ((double)((tiles + S - 1) / S) * tile_us + start_us);
+    if (S > 1) cost += 5.0 + (double)nrow * S * (8.0 * d + 16.0) / 4e6;
     if (S == 1 || cost < 0.95 * best_cost) best = S, best_cost = cost;
   }
   if (best > 1) *bytes = (size_t)nrow * best * (d * 4 + 8);
