@@ -32,6 +32,10 @@ struct Part {
   float2 *ml;  // [nsplit, rows]; null without splits
 };
 
+// Values from the caller's arrays are the same for all lanes, but loaded like any others: this makes them
+// known as uniform, and the branches and loops on them scalar.
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // Key tiles (KT keys each) of the rows of tokens i0..i1: nb bank tiles, a1 tiles of the
 // first tokens, then the window's tiles from b0.  hi, lo: positions that any row sees.
 struct Plan {
@@ -48,6 +52,9 @@ __device__ __forceinline__ Plan plan_of(const Mask &mask, const BankRows &bank, 
   p.b0 = max(p.lo / KT, p.a1);
   p.total = p.nb + p.a1 + max(0, (p.hi + KT - 1) / KT - p.b0);
   return p;
+}
+__device__ __forceinline__ Plan uni(const Plan &p) {
+  return Plan{uni(p.nb), uni(p.a1), uni(p.b0), uni(p.total), uni(p.hi), uni(p.lo), uni(p.m)};
 }
 __device__ __forceinline__ int tile_pos(const Plan &p, int KT, int t) {
   const int u = t - p.nb;
@@ -66,35 +73,51 @@ __device__ __forceinline__ void split_range(int total, int used, int split, int 
   t1 = min(total, t0 + per);
 }
 
-// Page numbers of 128 consecutive columns of a sequence's table, 64 in each of two
-// registers of a wave (one per lane), the second on its way while the first is used.
+// s_waitcnt immediate: at most n vector-memory operations and no LDS operation outstanding.
+constexpr int waitcnt_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
+__device__ __forceinline__ void stage_barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// Page numbers of 64 consecutive columns of a sequence's table in a register of a wave (one
+// per lane), and of the 64 after them on their way to LDS: values in flight in a register
+// would make the compiler wait for all loads wherever the register is moved.
 struct PageWindow {
   const int32_t *row;
-  int cols, P, base, cur, nxt;
-  __device__ __forceinline__ int load(int c0) const {
-    const int col = c0 + (int)(threadIdx.x & 63);
-    const int p = col < cols ? row[col] : -1;
-    return (unsigned)p < (unsigned)P ? p : -1;
+  int *next;  // 64 entries, of this wave
+  int cols, P, base, cur;
+  __device__ __forceinline__ int clamped(int c0) const {  // columns past the table repeat its last one: never asked for
+    return min(c0 + (int)(threadIdx.x & 63), cols - 1);
   }
-  __device__ __forceinline__ void init(const Pages &c, int s) {
+  __device__ __forceinline__ void init(const Pages &c, int s, int *lds) {
     row = c.table + (size_t)s * c.cols;
     cols = c.cols;
     P = c.P;
+    next = lds;
     base = -256;
+    cur = -1;
   }
   // columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page)
   __device__ __forceinline__ void seek(int col) {
     if (col >= base && col < base + 64) return;
     if (col >= base + 64 && col < base + 128) {
-      cur = nxt;
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      asm volatile("" ::: "memory");
+      cur = next[threadIdx.x & 63];
       base += 64;
     } else {
       base = col & ~63;
-      cur = load(base);
+      cur = row[clamped(base)];
     }
-    nxt = load(base + 64);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+    asm volatile("" ::: "memory");
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)row, (short)0, 4 * cols, kBufferRsrcWord3);
+    const int off = 4 * clamped(base + 64);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)next, 4, off, 0, 0, 0);
   }
-  __device__ __forceinline__ int page(int col) const { return __builtin_amdgcn_readlane(cur, col - base); }
+  // -1 if absent; the number comes from the caller's array and is bounded here
+  __device__ __forceinline__ int page(int col) const {
+    const int p = __builtin_amdgcn_readlane(cur, col - base);
+    return (unsigned)p < (unsigned)P ? p : -1;
+  }
 };
 
 // Physical 16-byte chunk of logical chunk c of row r (K: conflict-free 16-byte reads of
@@ -134,10 +157,10 @@ template <int D>
 __device__ __forceinline__ void rows8_issue(int rsub, int pc, const int *voff, const unsigned char *kp,
                                             const unsigned char *vp, int valid, int r0, char *kt, char *vt) {
   constexpr int RPL = 512 / D;
-  const __amdgpu_buffer_rsrc_t rk =
-      __builtin_amdgcn_make_buffer_rsrc((void *)kp, (short)0, valid * (2 * D), kBufferRsrcWord3);
-  const __amdgpu_buffer_rsrc_t rv =
-      __builtin_amdgcn_make_buffer_rsrc((void *)vp, (short)0, valid * (2 * D), kBufferRsrcWord3);
+  // uniform: the clamp to 0..8 would otherwise leave it in a vector register, and each load in a loop over its values
+  const int extent = __builtin_amdgcn_readfirstlane(valid) * (2 * D);
+  const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)kp, (short)0, extent, kBufferRsrcWord3);
+  const __amdgpu_buffer_rsrc_t rv = __builtin_amdgcn_make_buffer_rsrc((void *)vp, (short)0, extent, kBufferRsrcWord3);
 #pragma unroll
   for (int q = 0; q < Rows8<D>::kLoads; ++q) {
     const int r = q * RPL + rsub, koff = r * (2 * D) + 16 * k_swz<D>(r0 + r, pc);
@@ -148,50 +171,55 @@ __device__ __forceinline__ void rows8_issue(int rsub, int pc, const int *voff, c
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void *)(vt + r0 * (2 * D) + q * 1024), 16, voff[q], 0, 0, 0);
 }
 
-// A quarter row (D / 4 elements) on its way from memory to an LDS tile through registers.
+// A quarter of a quantised row on its way from memory to an LDS tile through registers: of
+// each run of four pieces of a row a lane takes its own, so that four lanes read 64 bytes
+// in a row.  The loads are buffer loads whose extent ends after the valid rows (the others
+// are zeros): without branches the compiler can count the loads in flight.
 template <int FMT, int D>
 struct Quarter {
-  u32x4 x[FMT == DKV_CACHE_FP8 ? D / 64 : 1];
-  int code;
-  __device__ __forceinline__ void load(const unsigned char *pool, const uint8_t *scale, size_t row, int part, bool ok) {
-    code = kScaleBias;
-    x[0] = u32x4{0, 0, 0, 0};
-    if constexpr (FMT == DKV_CACHE_FP8) {
-      if constexpr (D == 128) x[1] = u32x4{0, 0, 0, 0};
-      if (ok) {
-        const u32x4 *p = reinterpret_cast<const u32x4 *>(pool + row * D + part * (D / 4));
-        x[0] = p[0];
-        if constexpr (D == 128) x[1] = p[1];
-      }
-    } else {
-      if (ok) {
-        const unsigned char *p = pool + row * (D / 2) + part * (D / 8);
-        if constexpr (D == 128) {
-          x[0] = *reinterpret_cast<const u32x4 *>(p);
-        } else {
-          const u32x2 y = *reinterpret_cast<const u32x2 *>(p);
-          x[0] = u32x4{y[0], y[1], 0, 0};
-        }
+  static constexpr int kRow = FMT == DKV_CACHE_FP8 ? D : D / 2;                // bytes of a row
+  static constexpr int kPiece = kRow == 32 ? 8 : 16;                           // bytes
+  static constexpr int kElems = FMT == DKV_CACHE_FP8 ? kPiece : 2 * kPiece;    // elements of a piece
+  static constexpr int kPieces = kRow / (4 * kPiece);
+  u32x4 x[kPieces];
+  uint32_t codes;  // of the whole row
+  // base, scale: the first of the group's rows; r, part: this lane's row and piece
+  __device__ __forceinline__ void load(const unsigned char *base, const uint8_t *scale, int valid, int r, int part) {
+    const int n = __builtin_amdgcn_readfirstlane(valid);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void *)base, (short)0, n * kRow, kBufferRsrcWord3);
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc((void *)scale, (short)0, n * (D / kGroup), kBufferRsrcWord3);
+    const int at = r * kRow + part * kPiece, sat = r * (D / kGroup);
+#pragma unroll
+    for (int e = 0; e < kPieces; ++e) {
+      if constexpr (kPiece == 16) {
+        x[e] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, at + 64 * e, 0, 0));
+      } else {
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rx, at + 32 * e, 0, 0));
+        x[e] = u32x4{y[0], y[1], 0, 0};
       }
     }
-    if (ok) code = scale[row * (D / kGroup) + part * (D / 4) / kGroup];
+    if constexpr (D == 128) codes = __builtin_amdgcn_raw_buffer_load_b32(rs, sat, 0, 0);
+    else codes = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, sat, 0, 0);
   }
   template <bool V>
   __device__ __forceinline__ void store(char *tile, int r, int part) const {
+    asm volatile("" : "+v"(r), "+v"(part));  // addresses computed here, not kept in registers over the loop
 #pragma unroll
-    for (int e = 0; e < D / 32; ++e) {
-      uint4 y;
-      if constexpr (FMT == DKV_CACHE_FP8) y = bf16_of_fp8(uint2{x[e / 2][2 * (e & 1)], x[e / 2][2 * (e & 1) + 1]}, code);
-      else y = bf16_of_fp4(x[0][e], code);
-      const int ch = part * (D / 32) + e;
-      *reinterpret_cast<uint4 *>(tile + r * (2 * D) + 16 * (V ? v_swz<D>(r, ch) : k_swz<D>(r, ch))) = y;
+    for (int e = 0; e < kPieces; ++e) {
+      const int first = (4 * e + part) * kElems;
+      const int code = (int)(codes >> (8 * (first / kGroup))) & 255;
+#pragma unroll
+      for (int j = 0; j < kElems / 8; ++j) {
+        uint4 y;
+        if constexpr (FMT == DKV_CACHE_FP8) y = bf16_of_fp8(uint2{x[e][2 * j], x[e][2 * j + 1]}, code);
+        else y = bf16_of_fp4(x[e][j], code);
+        const int ch = first / 8 + j;
+        *reinterpret_cast<uint4 *>(tile + r * (2 * D) + 16 * (V ? v_swz<D>(r, ch) : k_swz<D>(r, ch))) = y;
+      }
     }
   }
 };
-
-// s_waitcnt immediate: at most n vector-memory operations and no LDS operation outstanding.
-constexpr int waitcnt_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
-__device__ __forceinline__ void stage_barrier() { asm volatile("s_barrier" ::: "memory"); }
 
 // Whether this lane or the row's other lane says so (every lane takes part in the exchange).
 __device__ __forceinline__ bool either_half(bool x) {
@@ -390,11 +418,11 @@ __device__ __forceinline__ void zero_nonfinite(char *vt) {
 }
 
 // In a tile that some rows see in part, a NaN or an infinity of V would reach the others
-// through 0 x inf.  Such values are added to the rows that see them (vis: bit k of a lane
-// for key k + 4 h of its row), as sums of the kinds that a row sees, and become zeros in
+// through 0 x inf.  Such values are added to the rows that see them (vis: as from
+// visible_bits), as sums of the kinds that a row sees, and become zeros in
 // the tile.  NT threads share the tile (all of them call this), one wave or a workgroup.
 template <int D, int NSUB, int NT>
-__device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool work) {
+__device__ __forceinline__ void purge(Rows<D> &r, char *vt, const uint32_t *vis, bool work) {
   constexpr int kBytes = NSUB * 32 * 2 * D;
   if (!has_nonfinite<kBytes>(vt)) return;
   if (work) {
@@ -404,7 +432,7 @@ __device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool w
 #pragma unroll 1
       for (int st = 0; st < 2 * NSUB; ++st) {
         u32x4 a = v_operand<D>(vt, st >> 1, st & 1, t2), bv;
-        const uint32_t w = (uint32_t)(vis >> (16 * st));
+        const uint32_t w = (NSUB > 1 && st >= 2 ? vis[NSUB - 1] : vis[0]) >> (16 * (st & 1));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           a[e] = kind_of(a[e] & 0xffffu) | (kind_of(a[e] >> 16) << 16);
@@ -431,6 +459,19 @@ __device__ __forceinline__ void purge(Rows<D> &r, char *vt, uint64_t vis, bool w
   if constexpr (NT > 64) stage_barrier();
 }
 
+// Bit j set where keys 8 j .. 8 j + 7 of the tile of KT tokens at pos lie in a page that is there.
+constexpr uint32_t kAllPresent = 0xffu;
+template <int KT>
+__device__ __forceinline__ uint32_t present_keys(const PageWindow &pw, int pos, int lps) {
+  uint32_t bits = KT == 64 ? 0u : kAllPresent & ~0xfu;
+  if ((1 << lps) >= KT) {
+    bits = pw.page(pos >> lps) >= 0 ? kAllPresent : 0u;
+  } else {
+#pragma unroll
+    for (int j = 0; j < KT / 16; ++j) bits |= (pw.page((pos + 16 * j) >> lps) >= 0 ? 3u : 0u) << (2 * j);
+  }
+  return __builtin_amdgcn_readfirstlane(bits);
+}
 // Which of the wave's rows see which keys of a tile.
 struct WaveMask {
   Seen first, last, row;  // of the wave's first and last row, and of this lane's
@@ -443,25 +484,28 @@ struct WaveMask {
   }
 };
 
-// Bits below x of 64.
-__device__ __forceinline__ uint64_t bits_below(int x) { return x <= 0 ? 0 : (x >= 64 ? ~0ull : (1ull << x) - 1); }
+// Bits below x of 32.
+__device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? ~0u : (1u << x) - 1u); }
 
-// Keys of the tile at pos that this lane's row sees, bit k for key k + 4 g (so that the bits
-// of the lane's score registers are in the same places for every lane group g); present: the
-// tile's keys in pages that are there.
-__device__ __forceinline__ uint64_t visible_bits(const WaveMask &w, int pos, uint64_t present, int g) {
-  const uint64_t m = bits_below(w.row.hi - pos) & (~bits_below(w.row.lo - pos) | bits_below(w.sink - pos)) & present;
+// Which of the 32 keys at pos this lane's row sees, bit k for key k + 4 g (so that the bits of
+// the lane's score registers are in the same places for every lane group g); present: of
+// these keys, four bits as from present_keys.
+__device__ __forceinline__ uint32_t visible_bits(const WaveMask &w, int pos, uint32_t present, int g) {
+  const uint32_t there = (((present & 15u) * 0x00204081u) & 0x01010101u) * 255u;  // bit j to byte j
+  const uint32_t m = bits_below(w.row.hi - pos) & (~bits_below(w.row.lo - pos) | bits_below(w.sink - pos)) & there;
   return m >> (4 * g);
 }
 template <int NSUB>
-__device__ __forceinline__ bool mask_cache(f32x16 *sc, uint64_t vis) {
-  constexpr uint64_t mine = NSUB == 2 ? 0x0f0f0f0f0f0f0f0full : 0x0f0f0f0full;
+__device__ __forceinline__ bool mask_cache(f32x16 *sc, const uint32_t *vis) {
+  uint32_t some = 0;
 #pragma unroll
-  for (int sub = 0; sub < NSUB; ++sub)
+  for (int sub = 0; sub < NSUB; ++sub) {
+    some |= vis[sub];
 #pragma unroll
     for (int i = 0; i < 16; ++i)
-      if (!((uint32_t)(vis >> (32 * sub)) & (1u << (8 * (i >> 2) + (i & 3))))) sc[sub][i] = -INFINITY;
-  return (vis & mine) != 0;
+      if (!(vis[sub] & (1u << (8 * (i >> 2) + (i & 3))))) sc[sub][i] = -INFINITY;
+  }
+  return (some & 0x0f0f0f0fu) != 0;
 }
 template <int NSUB>
 __device__ __forceinline__ void mask_bank(f32x16 *sc, int nvalid) {
@@ -471,17 +515,6 @@ __device__ __forceinline__ void mask_bank(f32x16 *sc, int nvalid) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (32 * sub + 8 * (i >> 2) + 4 * h + (i & 3) >= nvalid) sc[sub][i] = -INFINITY;
-}
-
-// Bits of the keys of the tile of KT tokens at pos that lie in pages that are there.
-template <int KT>
-__device__ __forceinline__ uint64_t present_keys(const PageWindow &pw, int pos, int lps) {
-  const int c0 = pos >> lps;
-  if ((1 << lps) >= KT) return pw.page(c0) >= 0 ? ~0ull : 0ull;
-  uint64_t bits = 0;
-  for (int j = 0; j < KT >> lps; ++j)
-    if (pw.page(c0 + j) >= 0) bits |= ((1ull << (1 << lps)) - 1) << (j << lps);
-  return KT == 64 ? bits : (bits | ~0xffffffffull);
 }
 
 // Row r (token, head of the group) of a row block -> its packed row and query head.
@@ -523,19 +556,21 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
   const int rb = nrb - 1 - p % nrb, bs = p / nrb, b = bs / nsplit, split = bs % nsplit;
   const int s = b / c.H, h = b % c.H;
-  const NewRows nr = new_rows(c, s);
+  const NewRows raw = new_rows(c, s), nr{uni(raw.first), uni(raw.n)};
   const int nrows = min(nr.n, c.max_new) * qs.G, r0 = rb * kWRows;
   if (r0 >= nrows) return;
-  const int len = seq_length(c, s);
+  const int len = uni(seq_length(c, s));
   const int r1 = min(r0 + kWRows, nrows) - 1;
-  const Plan pl = plan_of<kWK>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G);
+  const Plan pl = uni(plan_of<kWK>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G));
   const int used = splits_used<kWLeast>(pl.total, nsplit);
   if (split >= used) return;
   int tb, nt;
   split_range(pl.total, used, split, tb, nt);
+  tb = uni(tb), nt = uni(nt);
 
   __shared__ __attribute__((aligned(1024))) char k0[TB], k1[TB], k2[TB];
   __shared__ __attribute__((aligned(1024))) char v0[TB], v1[TB], v2[TB];
+  __shared__ __attribute__((aligned(256))) int pages_lds[64 * kWWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
   const int w0 = r0 + 32 * wave;
   const bool work = w0 < nrows;  // a wave past the last row only loads
@@ -544,6 +579,8 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const bool rv = w0 + n < nrows;
   bf16x8 qf[D / 16];
   load_q<D>(qf, qs, at, rv);
+  // here, so that no use of a query inside the loops waits for the tiles on their way
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
   Rows<D> rows;
   rows.init();
   WaveMask wm;
@@ -552,19 +589,19 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   wm.first = seen_by(mask, len, nr.n, min(w0, nrows - 1) / qs.G);
   wm.last = seen_by(mask, len, nr.n, min(w0 + 31, nrows - 1) / qs.G);
   PageWindow pw;   // of the tile being loaded
-  pw.init(c, s);
+  pw.init(c, s, pages_lds + 64 * wave);
 
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (2 * D);
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (2 * D);
 
   const Seen bfirst = seen_by(mask, len, nr.n, r0 / qs.G), blast = seen_by(mask, len, nr.n, r1 / qs.G);
-  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t present) __attribute__((always_inline)) {
     const int pos = tile_pos(pl, kWK, t);
     const bool act = work && (isbank || !wm.none(pos, kWK));
     // whether every row of the workgroup sees all of the tile: the same for all its waves
-    const bool whole = isbank || (present == ~0ull && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
+    const bool whole = isbank || (present == kAllPresent && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
     uint32_t pb[2][8];
-    uint64_t vis = 0;
+    uint32_t vis[2] = {0, 0};
     if (act) {
       f32x16 sc[2];
       scores<D, 2>(kt, qf, sc);
@@ -575,7 +612,8 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       } else if (whole) {
         rows.any = true;
       } else {
-        vis = visible_bits(wm, pos, present, lh);
+        vis[0] = visible_bits(wm, pos, present, lh);
+        vis[1] = visible_bits(wm, pos + 32, present >> 4, lh);
         rows.any |= mask_cache<2>(sc, vis);
       }
       softmax_update<D, 2>(rows, sc, pb, qs.scale_log2);
@@ -588,40 +626,48 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   // tiles in flight while one is used.  A wave loads 8 rows of each tile, which lie in one page.
   const Rows8<D> ld = rows8_offsets<D>();
   auto run_direct = [&](int t0, int t1) __attribute__((always_inline)) {
-    uint64_t pr[3] = {0, 0, 0};
-    auto issue = [&](int t, char *kd, char *vd) -> uint64_t {
-      if (t >= t1) return 0;
-      if (!FULL || t < pl.nb) {
-        const int r8 = t * kWK + 8 * wave;
-        rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(pl.m - r8, 0, 8),
-                       8 * wave, kd, vd);
-        return ~0ull;
+    uint32_t pr[3] = {0, 0, 0};
+    // Every call has the same number of loads (behind the last tile they read nothing and leave
+    // zeros), so that the waits can count them.
+    auto issue = [&](int t, char *kd, char *vd) __attribute__((always_inline)) -> uint32_t {
+      const unsigned char *kp = bk, *vp = bv;
+      int valid = 0;
+      uint32_t present = kAllPresent;
+      if (t < t1) {
+        if (!FULL || t < pl.nb) {
+          const int r8 = t * kWK + 8 * wave;
+          kp = bk + (size_t)r8 * (2 * D), vp = bv + (size_t)r8 * (2 * D);
+          valid = bound(pl.m - r8, 0, 8);
+        } else {
+          const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
+          pw.seek(pos >> c.lps);
+          const int page = pw.page(p8 >> c.lps);
+          if (page >= 0 && (p8 + 8 > pl.lo || p8 < mask.sink)) valid = bound(pl.hi - p8, 0, 8);
+          const size_t row = pool_row(c, max(page, 0), h, p8);
+          kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
+          present = present_keys<kWK>(pw, pos, c.lps);
+        }
       }
-      const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
-      pw.seek(pos >> c.lps);
-      const int page = pw.page(p8 >> c.lps);
-      int nv = bound(pl.hi - p8, 0, 8);
-      if (page < 0 || (p8 + 8 <= pl.lo && p8 >= mask.sink)) nv = 0;
-      const size_t row = pool_row(c, page < 0 ? 0 : page, h, p8);
-      rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * wave, kd, vd);
-      return present_keys<kWK>(pw, pos, c.lps);
+      rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * wave, kd, vd);
+      return present;
     };
     constexpr int kTileLoads = 2 * Rows8<D>::kLoads;
-    auto step = [&](int t, const char *kt, char *vt, uint64_t present, char *kn, char *vn) __attribute__((always_inline)) {
-      if (t + 1 < t1) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
-      else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+    auto step = [&](int t, const char *kt, char *vt, uint32_t present, char *kn, char *vn) __attribute__((always_inline)) {
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));  // the next tile may still be on its way
       stage_barrier();
-      const uint64_t nx = issue(t + 2, kn, vn);
-      compute(!FULL || t < pl.nb, t, kt, vt, present);
+      const uint32_t nx = issue(t + 2, kn, vn);
+      if (t < t1) compute(!FULL || t < pl.nb, t, kt, vt, present);
       return nx;
     };
     pr[0] = issue(t0, k0, v0);
     pr[1] = issue(t0 + 1, k1, v1);
+    // whole rounds of the stages, so that the loads in flight are the same wherever a round begins
     for (int t = t0; t < t1; t += 3) {
       pr[2] = step(t, k0, v0, pr[0], k2, v2);
-      if (t + 1 < t1) pr[0] = step(t + 1, k1, v1, pr[1], k0, v0);
-      if (t + 2 < t1) pr[1] = step(t + 2, k2, v2, pr[2], k1, v1);
+      pr[0] = step(t + 1, k1, v1, pr[1], k0, v0);
+      pr[1] = step(t + 2, k2, v2, pr[2], k1, v1);
     }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // nothing is on its way to the stages
   };
   if constexpr (FULL) {
     run_direct(tb, nt);
@@ -629,7 +675,6 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     const int t0 = max(tb, min(nt, pl.nb));
     if (tb < t0) {
       run_direct(tb, t0);
-      __builtin_amdgcn_s_waitcnt(0xc07f);
       stage_barrier();
     }
     // Quantised rows come through registers, two tiles ahead, and are stored as bf16: waves 0-3
@@ -639,47 +684,51 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
     struct {
       Quarter<FMT, D> x;
-      uint64_t present;
+      uint32_t present;
     } f[2];
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
-      if (t >= nt) return;
-      const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
-      pw.seek(pos >> c.lps);
-      const int page = pw.page(p16 >> c.lps);
-      const bool ok = page >= 0 && pos + lr < pl.hi && (p16 + 16 > pl.lo || p16 < mask.sink);
-      const size_t row = pool_row(c, page < 0 ? 0 : page, h, pos + lr);
-      y.x.load(isv ? c.v : c.k, isv ? c.vs : c.ks, row, qpart, ok);
-      y.present = present_keys<kWK>(pw, pos, c.lps);
+      size_t row = 0;
+      int valid = 0;
+      y.present = kAllPresent;
+      if (t < nt) {
+        const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
+        pw.seek(pos >> c.lps);
+        const int page = pw.page(p16 >> c.lps);
+        if (page >= 0 && (p16 + 16 > pl.lo || p16 < mask.sink)) valid = bound(pl.hi - p16, 0, 16);
+        row = pool_row(c, max(page, 0), h, p16);
+        y.present = present_keys<kWK>(pw, pos, c.lps);
+      }
+      y.x.load((isv ? c.v : c.k) + row * Quarter<FMT, D>::kRow, (isv ? c.vs : c.ks) + row * (D / kGroup), valid, l >> 2, qpart);
     };
-    uint64_t present = 0;
+    uint32_t present = 0;
     auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
-      const uint64_t now = present, next = y.present;
-      if (!isv && t + 1 < nt) {
-        y.x.template store<false>(kn, lr, qpart);
-        fetch(y, t + 3);
-      }
-      compute(false, t, kt, vt, now);
-      if (isv && t + 1 < nt) {
-        y.x.template store<true>(vn, lr, qpart);
-        fetch(y, t + 3);
-      }
+      const uint32_t now = present, next = y.present;
+      if (!isv) y.x.template store<false>(kn, lr, qpart);
+      if (t < nt) compute(false, t, kt, vt, now);
+      if (isv) y.x.template store<true>(vn, lr, qpart);
+      asm volatile("" ::: "memory");
+      fetch(y, t + 3);
+      asm volatile("" ::: "memory");
       present = next;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
       stage_barrier();
     };
     if (t0 < nt) {
       fetch(f[0], t0);
+      asm volatile("" ::: "memory");  // the loads in this order, which the waits count on
       fetch(f[1], t0 + 1);
+      asm volatile("" ::: "memory");
       if (isv) f[0].x.template store<true>(v0, lr, qpart);
       else f[0].x.template store<false>(k0, lr, qpart);
       present = f[0].present;
+      asm volatile("" ::: "memory");
       fetch(f[0], t0 + 2);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       stage_barrier();
     }
     for (int t = t0; t < nt; t += 2) {
       step(t, f[1], k0, v0, k1, v1);
-      if (t + 1 < nt) step(t + 1, f[0], k1, v1, k0, v0);
+      step(t + 1, f[0], k1, v1, k0, v0);
     }
   }
   if (!work) return;
@@ -737,7 +786,7 @@ struct Wave16 {
     return u32x4{a[0], a[1], b[0], b[1]};
   }
   // One tile: nvalid keys (bank tiles), or the keys of vis where not `whole`.
-  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint64_t vis) {
+  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint32_t vis) {
     const int l = threadIdx.x & 63, g = l >> 4, n = l & 15;
     f32x4 sc[2];
 #pragma unroll
@@ -757,7 +806,7 @@ struct Wave16 {
       for (int st = 0; st < 2; ++st)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if ((uint32_t)vis & (1u << (16 * st + i))) some = true;
+          if (vis & (1u << (16 * st + i))) some = true;
           else sc[st][i] = -INFINITY;
         }
       any |= some;
@@ -812,13 +861,13 @@ struct Wave16 {
                                                      o[t], 0, 0, 0);
   }
   // As the function of that name for 32 rows.
-  __device__ __forceinline__ void purge(char *vt, uint64_t vis) {
+  __device__ __forceinline__ void purge(char *vt, uint32_t vis) {
     if (!has_nonfinite<64 * D>(vt)) return;
     u32x4 bv;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int k = 16 * (e >> 1) + 2 * (e & 1);
-      bv[e] = ((uint32_t)(vis >> k) & 1 ? 0x3f80u : 0u) | ((uint32_t)(vis >> (k + 1)) & 1 ? 0x3f800000u : 0u);
+      bv[e] = ((vis >> k) & 1 ? 0x3f80u : 0u) | ((vis >> (k + 1)) & 1 ? 0x3f800000u : 0u);
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) {
@@ -865,7 +914,7 @@ struct Wave32 {
     }
     r.init();
   }
-  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint64_t vis) {
+  __device__ __forceinline__ void step(const char *kt, char *vt, float c, int nvalid, bool whole, uint32_t vis) {
     f32x16 sc[1];
     uint32_t pb[1][8];
     scores<D, 1>(kt, qf, sc);
@@ -873,10 +922,10 @@ struct Wave32 {
       r.any = true;
       if (nvalid < 32) mask_bank<1>(sc, nvalid);
     } else {
-      r.any |= mask_cache<1>(sc, vis);
+      r.any |= mask_cache<1>(sc, &vis);
     }
     softmax_update<D, 1>(r, sc, pb, c);
-    if (!whole) purge<D, 1, 64>(r, vt, vis, true);
+    if (!whole) purge<D, 1, 64>(r, vt, &vis, true);
     product<D, 1>(r, pb, vt);
   }
   __device__ __forceinline__ float2 stats() const { return r.stats(); }
@@ -904,15 +953,17 @@ struct Block {
     const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
     const int rb = p % nrb, bs = p / nrb;
     b = bs / nsplit, split = bs % nsplit, s = b / c.H, h = b % c.H;
-    nr = new_rows(c, s);
+    const NewRows raw = new_rows(c, s);
+    nr = NewRows{uni(raw.first), uni(raw.n)};
     r0 = rb * R;
     here = min(R, min(nr.n, c.max_new) * qs.G - r0);
     if (here <= 0) return false;
-    len = seq_length(c, s);
-    pl = plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G);
+    len = uni(seq_length(c, s));
+    pl = uni(plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G));
     const int used = splits_used<kFLeast>(pl.total, nsplit);
     if (split >= used) return false;
     split_range(pl.total, used, split, tb, nt);
+    tb = uni(tb), nt = uni(nt);
     return true;
   }
   __device__ __forceinline__ WaveMask wave_mask(const Mask &mask, const CacheQueries &qs, int i) const {
@@ -921,11 +972,11 @@ struct Block {
   }
 };
 
-// The four waves' results (in LDS, 128 D bytes apart: R rows of D floats, 16-byte chunk j of row r at j ^ (r % 8); wml: maxima and
+// The four waves' results (in LDS, 16 rows of D floats a wave in lo, 16 more in hi; 16-byte chunk j of row r at j ^ (r % 8); wml: maxima and
 // sums) joined under their common maximum, and written out, or as partial results of a split call.  unit: the factor
 // of the maxima's unit to log2.
 template <int DT, int D, int R>
-__device__ __forceinline__ void join_waves(const char *lds, const float2 (*wml)[R], const Block<R> &k, const Pages &c,
+__device__ __forceinline__ void join_waves(const char *lo, const char *hi, const float2 (*wml)[R], const Block<R> &k, const Pages &c,
                                            const CacheQueries &qs, const Part &part, float unit) {
   for (int e = threadIdx.x; e < k.here * (D / 4); e += 64 * kFWaves) {
     const int rr = e / (D / 4), j = 4 * (e % (D / 4));
@@ -937,7 +988,7 @@ __device__ __forceinline__ void join_waves(const char *lds, const float2 (*wml)[
     for (int w = 0; w < kFWaves; ++w) {
       const float2 ml = wml[w][rr];
       const float f = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
-      const float4 x = *reinterpret_cast<const float4 *>(lds + 4 * (w * 32 * D + rr * D + (j ^ (4 * (rr % 8)))));
+      const float4 x = *reinterpret_cast<const float4 *>((rr < 16 ? lo : hi) + 4 * ((16 * w + rr % 16) * D + (j ^ (4 * (rr % 8)))));
       lt = __builtin_fmaf(ml.y, f, lt);
       a[0] = __builtin_fmaf(x.x, f, a[0]);
       a[1] = __builtin_fmaf(x.y, f, a[1]);
@@ -968,81 +1019,88 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
     Pages c, Mask mask, BankRows bank, CacheQueries qs, int nrb, int nsplit, Part part) {
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   constexpr int TB = kFK * 2 * D;  // one tile of K or V
-  // Stages of (K tile, V tile) per wave; the first holds the waves' results at the end.  Two arrays, so that
-  // reads of one are known not to wait for loads into the other.
-  __shared__ __attribute__((aligned(1024))) char st0[kFWaves * 2 * TB], st1[FULL ? kFWaves * 2 * TB : 16];
+  // Stages of a K and a V tile per wave; the first holds the waves' results at the end.  Arrays of their own, so
+  // that reads of one are known not to wait for loads into another.
+  __shared__ __attribute__((aligned(1024))) char k0[kFWaves * TB], v0[kFWaves * TB];
+  __shared__ __attribute__((aligned(1024))) char k1[FULL ? kFWaves * TB : 16], v1[FULL ? kFWaves * TB : 16];
   __shared__ float2 wml[kFWaves][R];
+  __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<R> k;
   if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l % R;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
   PageWindow pw;
-  pw.init(c, k.s);
+  pw.init(c, k.s, pages_lds + 64 * wave);
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)k.b * bank.cap * (2 * D);
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)k.b * bank.cap * (2 * D);
-  char *mine = st0 + wave * 2 * TB, *other = st1 + (FULL ? wave * 2 * TB : 0);
+  char *ka = k0 + wave * TB, *va = v0 + wave * TB, *kb = k1 + (FULL ? wave * TB : 0), *vb = v1 + (FULL ? wave * TB : 0);
   std::conditional_t<R == 16, Wave16<D>, Wave32<D>> w;
   w.init(static_cast<const uint16_t *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh, n < k.here);
-  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint64_t present) __attribute__((always_inline)) {
+  // here, so that no use of a query inside the loops waits for the tiles on their way
+  __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t present) __attribute__((always_inline)) {
     const int pos = tile_pos(k.pl, kFK, t);
-    const bool whole = isbank || (present == ~0ull && wm.all(pos, kFK));
+    const bool whole = isbank || (present == kAllPresent && wm.all(pos, kFK));
     w.step(kt, vt, qs.scale_log2, isbank ? k.pl.m - t * kFK : kFK, whole, whole ? 0 : visible_bits(wm, pos, present, l / R));
   };
   const Rows8<D> ld = rows8_offsets<D>();
-  auto issue_bank = [&](int t, char *buf) __attribute__((always_inline)) {
+  // Loads of tile t, always the same number: behind the last tile they read nothing.
+  auto issue = [&](int t, char *kd, char *vd) __attribute__((always_inline)) -> uint32_t {
+    uint32_t present = kAllPresent;
+    const bool isbank = !FULL || t < k.pl.nb, in = t < k.nt;
+    const int pos = tile_pos(k.pl, kFK, t);
+    if (in && !isbank) {
+      pw.seek(pos >> c.lps);
+      present = present_keys<kFK>(pw, pos, c.lps);
+    }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int r8 = t * kFK + 8 * g;
-      rows8_issue<D>(ld.rsub, ld.pc, ld.v, bk + (size_t)r8 * (2 * D), bv + (size_t)r8 * (2 * D), bound(k.pl.m - r8, 0, 8),
-                     8 * g, buf, buf + TB);
+      const unsigned char *kp = bk, *vp = bv;
+      int valid = 0;
+      if (in) {
+        if (isbank) {
+          const int r8 = t * kFK + 8 * g;
+          kp = bk + (size_t)r8 * (2 * D), vp = bv + (size_t)r8 * (2 * D);
+          valid = bound(k.pl.m - r8, 0, 8);
+        } else {
+          const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
+          if (page >= 0 && (p8 + 8 > k.pl.lo || p8 < mask.sink)) valid = bound(k.pl.hi - p8, 0, 8);
+          const size_t row = pool_row(c, max(page, 0), k.h, p8);
+          kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
+        }
+      }
+      rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * g, kd, vd);
     }
+    return present;
   };
   if constexpr (FULL) {
     // two stages: a tile in flight while the other is used
-    auto issue = [&](int t, char *buf) -> uint64_t {
-      if (t >= k.nt) return 0;
-      if (t < k.pl.nb) {
-        issue_bank(t, buf);
-        return ~0ull;
-      }
-      const int pos = tile_pos(k.pl, kFK, t);
-      pw.seek(pos >> c.lps);
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
-        int nv = bound(k.pl.hi - p8, 0, 8);
-        if (page < 0 || (p8 + 8 <= k.pl.lo && p8 >= mask.sink)) nv = 0;
-        const size_t row = pool_row(c, page < 0 ? 0 : page, k.h, p8);
-        rows8_issue<D>(ld.rsub, ld.pc, ld.v, c.k + row * (2 * D), c.v + row * (2 * D), nv, 8 * g, buf, buf + TB);
-      }
-      return present_keys<kFK>(pw, pos, c.lps);
-    };
     constexpr int kTileLoads = 4 * 2 * Rows8<D>::kLoads;
-    auto step = [&](int t, char *buf, uint64_t present, char *next) __attribute__((always_inline)) {
-      const uint64_t nx = issue(t + kFWaves, next);
-      // this tile's loads are done, the next one's may be on their way
-      if (t + kFWaves < k.nt) __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));
-      else __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+    auto step = [&](int t, const char *kt, char *vt, uint32_t present, char *kn, char *vn) __attribute__((always_inline)) {
+      const uint32_t nx = issue(t + kFWaves, kn, vn);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));  // the next tile may still be on its way
       asm volatile("" ::: "memory");
-      compute(t < k.pl.nb, t, buf, buf + TB, present);
+      if (t < k.nt) compute(t < k.pl.nb, t, kt, vt, present);
       __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
       asm volatile("" ::: "memory");
       return nx;
     };
-    uint64_t p0 = issue(k.tb + wave, mine), p1 = 0;
-    for (int t = k.tb + wave; t < k.nt; t += 2 * kFWaves) {
-      p1 = step(t, mine, p0, other);
-      if (t + kFWaves < k.nt) p0 = step(t + kFWaves, other, p1, mine);
+    uint32_t p0 = issue(k.tb + wave, ka, va), p1 = 0;
+    for (int t = k.tb + wave; t < k.nt; t += 2 * kFWaves) {  // whole rounds of the stages, as in the other kernel
+      p1 = step(t, ka, va, p0, kb, vb);
+      p0 = step(t + kFWaves, kb, vb, p1, ka, va);
     }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // nothing is on its way to the stages
+    asm volatile("" ::: "memory");
   } else {
     // bank tiles one at a time: the other waves of the CU cover their latency
     int t = k.tb + wave;
     for (; t < min(k.nt, k.pl.nb); t += kFWaves) {
-      issue_bank(t, mine);
+      issue(t, ka, va);
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
       asm volatile("" ::: "memory");
-      compute(true, t, mine, mine + TB, ~0ull);
+      compute(true, t, ka, va, kAllPresent);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       asm volatile("" ::: "memory");
     }
@@ -1050,52 +1108,63 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
     // V, in rows l / 4 and 16 + l / 4
     struct {
       Quarter<FMT, D> k[2], v[2];
-      uint64_t present;
+      uint32_t present;
     } f[2];
     const int part4 = l & 3, lr = l >> 2;
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
-      if (t >= k.nt) return;
       const int pos = tile_pos(k.pl, kFK, t);
-      pw.seek(pos >> c.lps);
+      const bool in = t < k.nt;
+      y.present = kAllPresent;
+      if (in) {
+        pw.seek(pos >> c.lps);
+        y.present = present_keys<kFK>(pw, pos, c.lps);
+      }
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        const int p16 = pos + 16 * g, page = pw.page(p16 >> c.lps);
-        const bool ok = page >= 0 && p16 + lr < k.pl.hi && (p16 + 16 > k.pl.lo || p16 < mask.sink);
-        const size_t row = pool_row(c, page < 0 ? 0 : page, k.h, p16 + lr);
-        y.k[g].load(c.k, c.ks, row, part4, ok);
-        y.v[g].load(c.v, c.vs, row, part4, ok);
+        size_t row = 0;
+        int valid = 0;
+        if (in) {
+          const int p16 = pos + 16 * g, page = pw.page(p16 >> c.lps);
+          if (page >= 0 && (p16 + 16 > k.pl.lo || p16 < mask.sink)) valid = bound(k.pl.hi - p16, 0, 16);
+          row = pool_row(c, max(page, 0), k.h, p16);
+        }
+        y.k[g].load(c.k + row * Quarter<FMT, D>::kRow, c.ks + row * (D / kGroup), valid, lr, part4);
+        y.v[g].load(c.v + row * Quarter<FMT, D>::kRow, c.vs + row * (D / kGroup), valid, lr, part4);
       }
-      y.present = present_keys<kFK>(pw, pos, c.lps);
     };
     auto step = [&](auto &y, int t) __attribute__((always_inline)) {
       // the reads of the tile before are done: a wave's LDS operations run in order
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        y.k[g].template store<false>(mine, 16 * g + lr, part4);
-        y.v[g].template store<true>(mine + TB, 16 * g + lr, part4);
+        y.k[g].template store<false>(ka, 16 * g + lr, part4);
+        y.v[g].template store<true>(va, 16 * g + lr, part4);
       }
-      const uint64_t present = y.present;
+      const uint32_t present = y.present;
+      asm volatile("" ::: "memory");
       fetch(y, t + 2 * kFWaves);
+      asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
-      compute(false, t, mine, mine + TB, present);
+      if (t < k.nt) compute(false, t, ka, va, present);
       __builtin_amdgcn_wave_barrier();
     };
     fetch(f[0], t);
+    asm volatile("" ::: "memory");  // the loads in this order, which the waits count on
     fetch(f[1], t + kFWaves);
+    asm volatile("" ::: "memory");
     for (; t < k.nt; t += 2 * kFWaves) {
       step(f[0], t);
-      if (t + kFWaves < k.nt) step(f[1], t + kFWaves);
+      step(f[1], t + kFWaves);
     }
   }
 
   if (n < k.here) {
-    float *mo = reinterpret_cast<float *>(mine) + n * D;  // in the stages that only this wave uses
+    float *mo = reinterpret_cast<float *>(n < 16 ? ka : va) + (n % 16) * D;  // in the stages that only this wave uses
     const float2 ml = w.stats();
     if (l < R) wml[wave][n] = ml;
     w.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(mo + 4 * (chunk ^ (n % 8))) = x; });
   }
   __syncthreads();
-  join_waves<DKV_BF16, D, R>(st0, wml, k, c, qs, part, qs.scale_log2);
+  join_waves<DKV_BF16, D, R>(k0, v0, wml, k, c, qs, part, qs.scale_log2);
 }
 
 // fp32 scores and products on v_mfma_f32_32x32x2_f32, keys and values straight from memory.
@@ -1134,15 +1203,16 @@ __device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mask mask, BankRows bank, CacheQueries qs,
                                                                    int nrb, int nsplit, Part part) {
-  __shared__ __attribute__((aligned(16))) char st0[kFWaves * 32 * D * 4];  // the waves' results at the end
+  __shared__ __attribute__((aligned(16))) char lo[kFWaves * 64 * D], hi[kFWaves * 64 * D];  // the waves' results at the end
   __shared__ float2 wml[kFWaves][32];
+  __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<32> k;
   if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
   PageWindow pw;
-  pw.init(c, k.s);
+  pw.init(c, k.s, pages_lds + 64 * wave);
   Rows<D> rows;
   rows.init();
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)k.b * bank.cap * (4 * D);
@@ -1244,13 +1314,13 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mas
   }
 
   if (n < k.here) {
-    float *mo = reinterpret_cast<float *>(st0) + wave * 32 * D + n * D;
+    float *mo = reinterpret_cast<float *>(n < 16 ? lo : hi) + (16 * wave + n % 16) * D;
     const float2 ml = rows.stats();
     if (lh == 0) wml[wave][n] = ml;
     rows.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(mo + 4 * (chunk ^ (n % 8))) = x; });
   }
   __syncthreads();
-  join_waves<DKV_F32, D, 32>(st0, wml, k, c, qs, part, 1.0f);  // maxima in log2 units
+  join_waves<DKV_F32, D, 32>(lo, hi, wml, k, c, qs, part, 1.0f);  // maxima in log2 units
 }
 
 // Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  D / 4 lanes
