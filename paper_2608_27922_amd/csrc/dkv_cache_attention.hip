@@ -61,6 +61,71 @@ __device__ __forceinline__ int tile_pos(const Plan &p, int KT, int t) {
   return KT * (u < p.a1 ? u : u - p.a1 + p.b0);
 }
 
+// One piece of a call: row block rb of R rows of (sequence, kv head), key split `split`.
+struct Piece {
+  int s, h, rb, split;
+  NewRows nr;
+};
+// The piece of this workgroup; false where none is left.  The pieces of all sequences are numbered one after the other
+// (row blocks fastest), without gaps for sequences that have fewer than the longest, and each XCD (workgroup L runs on
+// XCD L % 8) takes an equal run of them: row blocks that read the same keys share an L2, and no XCD has more work than
+// the others.  (5 sequences of 388 to 777 tokens, 16 heads on 4: 107 us with a gap for every missing row block, which
+// gives some XCDs 33 pieces and others 22.)  Every wave takes part.
+template <int R>
+__device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs, int nsplit, Piece &w) {
+  const int l = threadIdx.x & 63, per = c.H * nsplit;
+  auto blocks = [&](int n) { return (min(n, c.max_new) * qs.G + R - 1) / R; };
+  int total = 0;
+  if (c.start && c.S > 1) {
+    for (int s0 = 0; s0 < c.S; s0 += 64) {
+      int n = s0 + l < c.S ? blocks(new_rows(c, s0 + l).n) : 0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
+      total += uni(n);
+    }
+  } else {
+    total = uni(c.S * blocks(new_rows(c, 0).n));
+  }
+  const unsigned N = (unsigned)total * per, L = blockIdx.x, xcd = L % 8;
+  if (L / 8 >= N / 8 + (xcd < N % 8 ? 1 : 0)) return false;
+  const unsigned p = xcd * (N / 8) + min(xcd, N % 8) + L / 8;
+  int u = (int)(p / per), first = 0, cnt;  // u: which row block of all, counted once per sequence
+  if (c.start && c.S > 1) {
+    for (int s0 = 0;; s0 += 64) {
+      const NewRows r = s0 + l < c.S ? new_rows(c, s0 + l) : NewRows{0, 0};
+      const int n = blocks(r.n);
+      int incl = n;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(incl, o, 64);
+        if (l >= o) incl += y;
+      }
+      const uint64_t later = __ballot(first + incl > u);
+      if (later == 0) {
+        first += __builtin_amdgcn_readlane(incl, 63);
+        continue;
+      }
+      const int i = __ffsll((unsigned long long)later) - 1;
+      w.s = s0 + i;
+      cnt = __builtin_amdgcn_readlane(n, i);
+      first += __builtin_amdgcn_readlane(incl, i) - cnt;
+      w.nr = NewRows{__builtin_amdgcn_readlane(r.first, i), __builtin_amdgcn_readlane(r.n, i)};
+      break;
+    }
+  } else {
+    cnt = total / c.S;
+    w.s = u / cnt;
+    first = w.s * cnt;
+    const NewRows r = new_rows(c, w.s);
+    w.nr = NewRows{uni(r.first), uni(r.n)};
+  }
+  const int rest = (int)(p - (unsigned)first * per), hs = rest / cnt;
+  w.rb = cnt - 1 - rest % cnt;  // later row blocks see more under a causal mask: first
+  w.h = hs / nsplit;
+  w.split = hs % nsplit;
+  return true;
+}
+
 // The host sizes the splits by the largest sequence; of them a row block takes as many as
 // leave each at least LEAST tiles (one at least), in equal runs.
 template <int LEAST>
@@ -82,8 +147,9 @@ __device__ __forceinline__ void stage_barrier() { asm volatile("s_barrier" ::: "
 // would make the compiler wait for all loads wherever the register is moved.
 struct PageWindow {
   const int32_t *row;
-  int *next;  // 64 entries, of this wave
+  int *next;      // 64 entries, of this wave
   int cols, P, base, cur;
+  uint64_t gone;  // bit i: column base + i is absent
   __device__ __forceinline__ int clamped(int c0) const {  // columns past the table repeat its last one: never asked for
     return min(c0 + (int)(threadIdx.x & 63), cols - 1);
   }
@@ -93,7 +159,8 @@ struct PageWindow {
     P = c.P;
     next = lds;
     base = -256;
-    cur = -1;
+    cur = 0;
+    gone = 0;
   }
   // columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page)
   __device__ __forceinline__ void seek(int col) {
@@ -109,15 +176,15 @@ struct PageWindow {
     }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     asm volatile("" ::: "memory");
+    gone = __ballot((unsigned)cur >= (unsigned)P);  // the numbers come from the caller's array and are bounded here
+    if ((unsigned)cur >= (unsigned)P) cur = 0;
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)row, (short)0, 4 * cols, kBufferRsrcWord3);
     const int off = 4 * clamped(base + 64);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void *)next, 4, off, 0, 0, 0);
   }
-  // -1 if absent; the number comes from the caller's array and is bounded here
-  __device__ __forceinline__ int page(int col) const {
-    const int p = __builtin_amdgcn_readlane(cur, col - base);
-    return (unsigned)p < (unsigned)P ? p : -1;
-  }
+  // Page of a column (any page if it is absent), and the absent ones of n columns, bit 0 the first.
+  __device__ __forceinline__ int page(int col) const { return __builtin_amdgcn_readlane(cur, col - base); }
+  __device__ __forceinline__ uint32_t absent(int col, int n) const { return (uint32_t)(gone >> (col - base)) & ((1u << n) - 1u); }
 };
 
 // Physical 16-byte chunk of logical chunk c of row r (K: conflict-free 16-byte reads of
@@ -459,19 +526,6 @@ __device__ __forceinline__ void purge(Rows<D> &r, char *vt, const uint32_t *vis,
   if constexpr (NT > 64) stage_barrier();
 }
 
-// Bit j set where keys 8 j .. 8 j + 7 of the tile of KT tokens at pos lie in a page that is there.
-constexpr uint32_t kAllPresent = 0xffu;
-template <int KT>
-__device__ __forceinline__ uint32_t present_keys(const PageWindow &pw, int pos, int lps) {
-  uint32_t bits = KT == 64 ? 0u : kAllPresent & ~0xfu;
-  if ((1 << lps) >= KT) {
-    bits = pw.page(pos >> lps) >= 0 ? kAllPresent : 0u;
-  } else {
-#pragma unroll
-    for (int j = 0; j < KT / 16; ++j) bits |= (pw.page((pos + 16 * j) >> lps) >= 0 ? 3u : 0u) << (2 * j);
-  }
-  return __builtin_amdgcn_readfirstlane(bits);
-}
 // Which of the wave's rows see which keys of a tile.
 struct WaveMask {
   Seen first, last, row;  // of the wave's first and last row, and of this lane's
@@ -488,10 +542,10 @@ struct WaveMask {
 __device__ __forceinline__ uint32_t bits_below(int x) { return x <= 0 ? 0u : (x >= 32 ? ~0u : (1u << x) - 1u); }
 
 // Which of the 32 keys at pos this lane's row sees, bit k for key k + 4 g (so that the bits of
-// the lane's score registers are in the same places for every lane group g); present: of
-// these keys, four bits as from present_keys.
-__device__ __forceinline__ uint32_t visible_bits(const WaveMask &w, int pos, uint32_t present, int g) {
-  const uint32_t there = (((present & 15u) * 0x00204081u) & 0x01010101u) * 255u;  // bit j to byte j
+// the lane's score registers are in the same places for every lane group g).  They are keys
+// first .. first + 31 of a tile of which absent (PageWindow) says the pages that are not there.
+__device__ __forceinline__ uint32_t visible_bits(const WaveMask &w, int pos, int first, uint32_t absent, int lps, int g) {
+  const uint32_t there = ((absent >> (first >> lps)) & 1 ? 0u : 0xffffu) | ((absent >> ((first + 16) >> lps)) & 1 ? 0u : 0xffff0000u);
   const uint32_t m = bits_below(w.row.hi - pos) & (~bits_below(w.row.lo - pos) | bits_below(w.sink - pos)) & there;
   return m >> (4 * g);
 }
@@ -547,18 +601,14 @@ constexpr int kWWaves = 8, kWRows = 32 * kWWaves, kWK = 64, kWLeast = 4;
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Mask mask, BankRows bank, CacheQueries qs,
-                                                                    int nrb, int nsplit, Part part) {
+                                                                    int nsplit, Part part) {
   constexpr int TB = kWK * 2 * D;
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
-  // Workgroup L runs on XCD L % 8: rank the workgroups XCD by XCD, so that the row blocks that
-  // read the same keys share an L2; the later row blocks (longest under a causal mask) first.
-  const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
-  const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
-  const int rb = nrb - 1 - p % nrb, bs = p / nrb, b = bs / nsplit, split = bs % nsplit;
-  const int s = b / c.H, h = b % c.H;
-  const NewRows raw = new_rows(c, s), nr{uni(raw.first), uni(raw.n)};
-  const int nrows = min(nr.n, c.max_new) * qs.G, r0 = rb * kWRows;
-  if (r0 >= nrows) return;
+  Piece w;
+  if (!my_piece<kWRows>(c, qs, nsplit, w)) return;
+  const int s = w.s, h = w.h, b = s * c.H + h, split = w.split;
+  const NewRows nr = w.nr;
+  const int nrows = min(nr.n, c.max_new) * qs.G, r0 = w.rb * kWRows;
   const int len = uni(seq_length(c, s));
   const int r1 = min(r0 + kWRows, nrows) - 1;
   const Plan pl = uni(plan_of<kWK>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G));
@@ -594,12 +644,13 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (2 * D);
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (2 * D);
 
+  const int kcols = max(1, kWK >> c.lps);  // pages that a tile lies in
   const Seen bfirst = seen_by(mask, len, nr.n, r0 / qs.G), blast = seen_by(mask, len, nr.n, r1 / qs.G);
-  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t present) __attribute__((always_inline)) {
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t absent) __attribute__((always_inline)) {
     const int pos = tile_pos(pl, kWK, t);
     const bool act = work && (isbank || !wm.none(pos, kWK));
     // whether every row of the workgroup sees all of the tile: the same for all its waves
-    const bool whole = isbank || (present == kAllPresent && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
+    const bool whole = isbank || (absent == 0 && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
     uint32_t pb[2][8];
     uint32_t vis[2] = {0, 0};
     if (act) {
@@ -612,8 +663,8 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       } else if (whole) {
         rows.any = true;
       } else {
-        vis[0] = visible_bits(wm, pos, present, lh);
-        vis[1] = visible_bits(wm, pos + 32, present >> 4, lh);
+        vis[0] = visible_bits(wm, pos, 0, absent, c.lps, lh);
+        vis[1] = visible_bits(wm, pos + 32, 32, absent, c.lps, lh);
         rows.any |= mask_cache<2>(sc, vis);
       }
       softmax_update<D, 2>(rows, sc, pb, qs.scale_log2);
@@ -632,7 +683,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     auto issue = [&](int t, char *kd, char *vd) __attribute__((always_inline)) -> uint32_t {
       const unsigned char *kp = bk, *vp = bv;
       int valid = 0;
-      uint32_t present = kAllPresent;
+      uint32_t absent = 0;
       if (t < t1) {
         if (!FULL || t < pl.nb) {
           const int r8 = t * kWK + 8 * wave;
@@ -641,22 +692,21 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
         } else {
           const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
           pw.seek(pos >> c.lps);
-          const int page = pw.page(p8 >> c.lps);
-          if (page >= 0 && (p8 + 8 > pl.lo || p8 < mask.sink)) valid = bound(pl.hi - p8, 0, 8);
-          const size_t row = pool_row(c, max(page, 0), h, p8);
+          if (!pw.absent(p8 >> c.lps, 1) && (p8 + 8 > pl.lo || p8 < mask.sink)) valid = bound(pl.hi - p8, 0, 8);
+          const size_t row = pool_row(c, pw.page(p8 >> c.lps), h, p8);
           kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
-          present = present_keys<kWK>(pw, pos, c.lps);
+          absent = pw.absent(pos >> c.lps, kcols);
         }
       }
       rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * wave, kd, vd);
-      return present;
+      return absent;
     };
     constexpr int kTileLoads = 2 * Rows8<D>::kLoads;
-    auto step = [&](int t, const char *kt, char *vt, uint32_t present, char *kn, char *vn) __attribute__((always_inline)) {
+    auto step = [&](int t, const char *kt, char *vt, uint32_t absent, char *kn, char *vn) __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));  // the next tile may still be on its way
       stage_barrier();
       const uint32_t nx = issue(t + 2, kn, vn);
-      if (t < t1) compute(!FULL || t < pl.nb, t, kt, vt, present);
+      if (t < t1) compute(!FULL || t < pl.nb, t, kt, vt, absent);
       return nx;
     };
     pr[0] = issue(t0, k0, v0);
@@ -684,32 +734,31 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
     struct {
       Quarter<FMT, D> x;
-      uint32_t present;
+      uint32_t absent;
     } f[2];
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
       size_t row = 0;
       int valid = 0;
-      y.present = kAllPresent;
+      y.absent = 0;
       if (t < nt) {
         const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
         pw.seek(pos >> c.lps);
-        const int page = pw.page(p16 >> c.lps);
-        if (page >= 0 && (p16 + 16 > pl.lo || p16 < mask.sink)) valid = bound(pl.hi - p16, 0, 16);
-        row = pool_row(c, max(page, 0), h, p16);
-        y.present = present_keys<kWK>(pw, pos, c.lps);
+        if (!pw.absent(p16 >> c.lps, 1) && (p16 + 16 > pl.lo || p16 < mask.sink)) valid = bound(pl.hi - p16, 0, 16);
+        row = pool_row(c, pw.page(p16 >> c.lps), h, p16);
+        y.absent = pw.absent(pos >> c.lps, kcols);
       }
       y.x.load((isv ? c.v : c.k) + row * Quarter<FMT, D>::kRow, (isv ? c.vs : c.ks) + row * (D / kGroup), valid, l >> 2, qpart);
     };
-    uint32_t present = 0;
+    uint32_t absent = 0;
     auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
-      const uint32_t now = present, next = y.present;
+      const uint32_t now = absent, next = y.absent;
       if (!isv) y.x.template store<false>(kn, lr, qpart);
       if (t < nt) compute(false, t, kt, vt, now);
       if (isv) y.x.template store<true>(vn, lr, qpart);
       asm volatile("" ::: "memory");
       fetch(y, t + 3);
       asm volatile("" ::: "memory");
-      present = next;
+      absent = next;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
       stage_barrier();
     };
@@ -720,7 +769,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       asm volatile("" ::: "memory");
       if (isv) f[0].x.template store<true>(v0, lr, qpart);
       else f[0].x.template store<false>(k0, lr, qpart);
-      present = f[0].present;
+      absent = f[0].absent;
       asm volatile("" ::: "memory");
       fetch(f[0], t0 + 2);
       __builtin_amdgcn_s_waitcnt(0xc07f);
@@ -945,19 +994,15 @@ struct Block {
   int s, h, b, split, len, here, r0, tb, nt;
   NewRows nr;
   Plan pl;
-  // False where it has nothing to do.  Workgroup L runs on XCD L % 8: the row blocks and splits of
-  // a (sequence, head) are ranked XCD by XCD.
-  __device__ __forceinline__ bool init(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, int nrb,
+  // False where it has nothing to do.
+  __device__ __forceinline__ bool init(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs,
                                        int nsplit) {
-    const int T = (int)gridDim.x, L = (int)blockIdx.x, xcd = L % 8;
-    const int p = xcd * (T / 8) + min(xcd, T % 8) + L / 8;
-    const int rb = p % nrb, bs = p / nrb;
-    b = bs / nsplit, split = bs % nsplit, s = b / c.H, h = b % c.H;
-    const NewRows raw = new_rows(c, s);
-    nr = NewRows{uni(raw.first), uni(raw.n)};
-    r0 = rb * R;
+    Piece w;
+    if (!my_piece<R>(c, qs, nsplit, w)) return false;
+    s = w.s, h = w.h, split = w.split, nr = w.nr;
+    b = s * c.H + h;
+    r0 = w.rb * R;
     here = min(R, min(nr.n, c.max_new) * qs.G - r0);
-    if (here <= 0) return false;
     len = uni(seq_length(c, s));
     pl = uni(plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G));
     const int used = splits_used<kFLeast>(pl.total, nsplit);
@@ -1016,7 +1061,7 @@ __device__ __forceinline__ void join_waves(const char *lo, const char *hi, const
 // R rows per workgroup: 16 or 32.
 template <int FMT, int D, int R>
 __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1 : 2) void k_cache_attn_few(
-    Pages c, Mask mask, BankRows bank, CacheQueries qs, int nrb, int nsplit, Part part) {
+    Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit, Part part) {
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   constexpr int TB = kFK * 2 * D;  // one tile of K or V
   // Stages of a K and a V tile per wave; the first holds the waves' results at the end.  Arrays of their own, so
@@ -1026,7 +1071,7 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
   __shared__ float2 wml[kFWaves][R];
   __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<R> k;
-  if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
+  if (!k.init(c, mask, bank, qs, nsplit)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l % R;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
@@ -1039,20 +1084,21 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
   w.init(static_cast<const uint16_t *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh, n < k.here);
   // here, so that no use of a query inside the loops waits for the tiles on their way
   __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
-  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t present) __attribute__((always_inline)) {
+  auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t absent) __attribute__((always_inline)) {
     const int pos = tile_pos(k.pl, kFK, t);
-    const bool whole = isbank || (present == kAllPresent && wm.all(pos, kFK));
-    w.step(kt, vt, qs.scale_log2, isbank ? k.pl.m - t * kFK : kFK, whole, whole ? 0 : visible_bits(wm, pos, present, l / R));
+    const bool whole = isbank || (absent == 0 && wm.all(pos, kFK));
+    w.step(kt, vt, qs.scale_log2, isbank ? k.pl.m - t * kFK : kFK, whole, whole ? 0 : visible_bits(wm, pos, 0, absent, c.lps, l / R));
   };
+  const int kcols = max(1, kFK >> c.lps);  // pages that a tile lies in
   const Rows8<D> ld = rows8_offsets<D>();
   // Loads of tile t, always the same number: behind the last tile they read nothing.
   auto issue = [&](int t, char *kd, char *vd) __attribute__((always_inline)) -> uint32_t {
-    uint32_t present = kAllPresent;
+    uint32_t absent = 0;
     const bool isbank = !FULL || t < k.pl.nb, in = t < k.nt;
     const int pos = tile_pos(k.pl, kFK, t);
     if (in && !isbank) {
       pw.seek(pos >> c.lps);
-      present = present_keys<kFK>(pw, pos, c.lps);
+      absent = pw.absent(pos >> c.lps, kcols);
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -1064,24 +1110,24 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
           kp = bk + (size_t)r8 * (2 * D), vp = bv + (size_t)r8 * (2 * D);
           valid = bound(k.pl.m - r8, 0, 8);
         } else {
-          const int p8 = pos + 8 * g, page = pw.page(p8 >> c.lps);
-          if (page >= 0 && (p8 + 8 > k.pl.lo || p8 < mask.sink)) valid = bound(k.pl.hi - p8, 0, 8);
-          const size_t row = pool_row(c, max(page, 0), k.h, p8);
+          const int p8 = pos + 8 * g;
+          if (!pw.absent(p8 >> c.lps, 1) && (p8 + 8 > k.pl.lo || p8 < mask.sink)) valid = bound(k.pl.hi - p8, 0, 8);
+          const size_t row = pool_row(c, pw.page(p8 >> c.lps), k.h, p8);
           kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
         }
       }
       rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * g, kd, vd);
     }
-    return present;
+    return absent;
   };
   if constexpr (FULL) {
     // two stages: a tile in flight while the other is used
     constexpr int kTileLoads = 4 * 2 * Rows8<D>::kLoads;
-    auto step = [&](int t, const char *kt, char *vt, uint32_t present, char *kn, char *vn) __attribute__((always_inline)) {
+    auto step = [&](int t, const char *kt, char *vt, uint32_t absent, char *kn, char *vn) __attribute__((always_inline)) {
       const uint32_t nx = issue(t + kFWaves, kn, vn);
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));  // the next tile may still be on its way
       asm volatile("" ::: "memory");
-      if (t < k.nt) compute(t < k.pl.nb, t, kt, vt, present);
+      if (t < k.nt) compute(t < k.pl.nb, t, kt, vt, absent);
       __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
       asm volatile("" ::: "memory");
       return nx;
@@ -1100,7 +1146,7 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
       issue(t, ka, va);
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
       asm volatile("" ::: "memory");
-      compute(true, t, ka, va, kAllPresent);
+      compute(true, t, ka, va, 0);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       asm volatile("" ::: "memory");
     }
@@ -1108,25 +1154,25 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
     // V, in rows l / 4 and 16 + l / 4
     struct {
       Quarter<FMT, D> k[2], v[2];
-      uint32_t present;
+      uint32_t absent;
     } f[2];
     const int part4 = l & 3, lr = l >> 2;
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
       const int pos = tile_pos(k.pl, kFK, t);
       const bool in = t < k.nt;
-      y.present = kAllPresent;
+      y.absent = 0;
       if (in) {
         pw.seek(pos >> c.lps);
-        y.present = present_keys<kFK>(pw, pos, c.lps);
+        y.absent = pw.absent(pos >> c.lps, kcols);
       }
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         size_t row = 0;
         int valid = 0;
         if (in) {
-          const int p16 = pos + 16 * g, page = pw.page(p16 >> c.lps);
-          if (page >= 0 && (p16 + 16 > k.pl.lo || p16 < mask.sink)) valid = bound(k.pl.hi - p16, 0, 16);
-          row = pool_row(c, max(page, 0), k.h, p16);
+          const int p16 = pos + 16 * g;
+          if (!pw.absent(p16 >> c.lps, 1) && (p16 + 16 > k.pl.lo || p16 < mask.sink)) valid = bound(k.pl.hi - p16, 0, 16);
+          row = pool_row(c, pw.page(p16 >> c.lps), k.h, p16);
         }
         y.k[g].load(c.k + row * Quarter<FMT, D>::kRow, c.ks + row * (D / kGroup), valid, lr, part4);
         y.v[g].load(c.v + row * Quarter<FMT, D>::kRow, c.vs + row * (D / kGroup), valid, lr, part4);
@@ -1139,12 +1185,12 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
         y.k[g].template store<false>(ka, 16 * g + lr, part4);
         y.v[g].template store<true>(va, 16 * g + lr, part4);
       }
-      const uint32_t present = y.present;
+      const uint32_t absent = y.absent;
       asm volatile("" ::: "memory");
       fetch(y, t + 2 * kFWaves);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
-      if (t < k.nt) compute(false, t, ka, va, present);
+      if (t < k.nt) compute(false, t, ka, va, absent);
       __builtin_amdgcn_wave_barrier();
     };
     fetch(f[0], t);
@@ -1202,12 +1248,12 @@ __device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mask mask, BankRows bank, CacheQueries qs,
-                                                                   int nrb, int nsplit, Part part) {
+                                                                   int nsplit, Part part) {
   __shared__ __attribute__((aligned(16))) char lo[kFWaves * 64 * D], hi[kFWaves * 64 * D];  // the waves' results at the end
   __shared__ float2 wml[kFWaves][32];
   __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<32> k;
-  if (!k.init(c, mask, bank, qs, nrb, nsplit)) return;
+  if (!k.init(c, mask, bank, qs, nsplit)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
@@ -1306,11 +1352,11 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mas
     const int pos = tile_pos(k.pl, kFK, t);
     pw.seek(pos >> c.lps);
     const int pa = pw.page(pos >> c.lps), pb = pw.page((pos + 16) >> c.lps);
-    uint32_t okbits = (pa >= 0 ? 0xffffu : 0u) | (pb >= 0 ? 0xffff0000u : 0u);
+    uint32_t okbits = (pw.absent(pos >> c.lps, 1) ? 0u : 0xffffu) | (pw.absent((pos + 16) >> c.lps, 1) ? 0u : 0xffff0000u);
     if (k.pl.hi - pos < 32) okbits &= (1u << (k.pl.hi - pos)) - 1u;
     // rows before the window of every row block's token and behind the first tokens are not read
     tile(std::integral_constant<int, FMT>(), t, c.k, c.ks, c.v, c.vs,
-         [&](int key) { return pool_row(c, max(key < 16 ? pa : pb, 0), k.h, pos + key); }, okbits);
+         [&](int key) { return pool_row(c, key < 16 ? pa : pb, k.h, pos + key); }, okbits);
   }
 
   if (n < k.here) {
@@ -1430,17 +1476,17 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
   const unsigned g = (unsigned)grid;
   if constexpr (DT == DKV_BF16) {
     if (R == kWRows) {
-      k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
       if (nsplit > 1) combine<DT, D, kWRows, kWK, kWLeast>(c, mask, bank, qs, nsplit, part, s);
     } else if (R == 32) {
-      k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
       if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
     } else {
-      k_cache_attn_few<FMT, D, 16><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+      k_cache_attn_few<FMT, D, 16><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
       if (nsplit > 1) combine<DT, D, 16, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
     }
   } else {
-    k_cache_attn_f32<FMT, D><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, (int)nrb, nsplit, part);
+    k_cache_attn_f32<FMT, D><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
     if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
   }
   return hipGetLastError();
