@@ -393,7 +393,7 @@ typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_ca
  */
 typedef struct {
   int32_t num_seqs;     /* S >= 1 */
-  int32_t num_kv_heads; /* H >= 1 */
+  int32_t num_kv_heads; /* H >= 1; k's part of a page (H * page_size rows) less than 2^31 bytes */
   int32_t head_dim;     /* 64 or 128 */
   int32_t page_size;    /* tokens per page: 16, 32, 64, 128 or 256 */
   int32_t num_pages;    /* P >= 1 */

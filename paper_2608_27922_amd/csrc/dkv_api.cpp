@@ -194,6 +194,10 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   if (c->num_seqs < 1 || c->num_kv_heads < 1 || c->num_pages < 1 || c->max_pages < 1) return DKV_ERR_SHAPE;
   if (((int64_t)c->max_pages << lps) > (int64_t(1) << 30)) return DKV_ERR_SHAPE;
   if ((int64_t)c->num_seqs * c->num_kv_heads >= (int64_t(1) << 24)) return DKV_ERR_SHAPE;
+  // bytes of a page are 32-bit numbers in the kernels
+  const int row = c->format == DKV_CACHE_FULL ? c->head_dim * (c->dtype == DKV_BF16 ? 2 : 4)
+                                              : (c->format == DKV_CACHE_FP8 ? c->head_dim : c->head_dim / 2);
+  if (((int64_t)c->num_kv_heads << lps) * row >= (int64_t(1) << 31)) return DKV_ERR_SHAPE;
   if (!c->k || !c->v || !c->page_table || !c->length) return DKV_ERR_INVALID;
   if (c->format != DKV_CACHE_FULL && (!c->k_scale || !c->v_scale)) return DKV_ERR_INVALID;
   if (!aligned16(c->k) || !aligned16(c->v)) return DKV_ERR_INVALID;

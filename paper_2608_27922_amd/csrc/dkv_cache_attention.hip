@@ -162,19 +162,22 @@ struct PageWindow {
     cur = 0;
     gone = 0;
   }
-  // columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page)
+  // Columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page).  Tiles ascend
+  // by at most 8 columns, so at least 16 loads of tiles have been issued after the load of `next` when it is needed:
+  // all but the 16 youngest loads being done, it is there, and the tiles on their way are not waited for.
   __device__ __forceinline__ void seek(int col) {
     if (col >= base && col < base + 64) return;
     if (col >= base + 64 && col < base + 128) {
-      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(16));
       asm volatile("" ::: "memory");
-      cur = next[threadIdx.x & 63];
+      cur = ((const __attribute__((address_space(3))) int *)next)[threadIdx.x & 63];
       base += 64;
+      __builtin_amdgcn_s_waitcnt(0xc07f);
     } else {
-      base = col & ~63;
+      base = col;
       cur = row[clamped(base)];
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     }
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     asm volatile("" ::: "memory");
     gone = __ballot((unsigned)cur >= (unsigned)P);  // the numbers come from the caller's array and are bounded here
     if ((unsigned)cur >= (unsigned)P) cur = 0;
@@ -185,6 +188,19 @@ struct PageWindow {
   // Page of a column (any page if it is absent), and the absent ones of n columns, bit 0 the first.
   __device__ __forceinline__ int page(int col) const { return __builtin_amdgcn_readlane(cur, col - base); }
   __device__ __forceinline__ uint32_t absent(int col, int n) const { return (uint32_t)(gone >> (col - base)) & ((1u << n) - 1u); }
+};
+
+// Byte offset in the pool of position pos of a head in a page: pages are less than 2^31 bytes (checked by the
+// caller), so only the page number takes a 64-bit product.
+struct PoolAt {
+  uint32_t page_bytes, head_bytes, mask;
+  int row;
+  __device__ __forceinline__ PoolAt(const Pages &c, int h, int row_bytes)
+      : page_bytes((uint32_t)(c.H << c.lps) * row_bytes), head_bytes((uint32_t)(h << c.lps) * row_bytes),
+        mask((1u << c.lps) - 1), row(row_bytes) {}
+  __device__ __forceinline__ size_t at(int page, int pos) const {
+    return (uint64_t)(uint32_t)page * page_bytes + (head_bytes + ((uint32_t)pos & mask) * row);
+  }
 };
 
 // Physical 16-byte chunk of logical chunk c of row r (K: conflict-free 16-byte reads of
@@ -676,6 +692,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   // Tiles [t0, t1) of rows held in bf16 go global -> LDS without registers, three stages: two
   // tiles in flight while one is used.  A wave loads 8 rows of each tile, which lie in one page.
   const Rows8<D> ld = rows8_offsets<D>();
+  const PoolAt pool(c, h, FULL ? 2 * D : Quarter<FULL ? DKV_CACHE_FP8 : FMT, D>::kRow);
   auto run_direct = [&](int t0, int t1) __attribute__((always_inline)) {
     uint32_t pr[3] = {0, 0, 0};
     // Every call has the same number of loads (behind the last tile they read nothing and leave
@@ -692,10 +709,13 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
         } else {
           const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
           pw.seek(pos >> c.lps);
-          if (!pw.absent(p8 >> c.lps, 1) && (p8 + 8 > pl.lo || p8 < mask.sink)) valid = bound(pl.hi - p8, 0, 8);
-          const size_t row = pool_row(c, pw.page(p8 >> c.lps), h, p8);
-          kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
-          absent = pw.absent(pos >> c.lps, kcols);
+          valid = 8;
+          if (pw.gone != 0 || pos < pl.lo || pos + kWK > pl.hi) {
+            absent = pw.absent(pos >> c.lps, kcols);
+            valid = !pw.absent(p8 >> c.lps, 1) && (p8 + 8 > pl.lo || p8 < mask.sink) ? bound(pl.hi - p8, 0, 8) : 0;
+          }
+          const size_t off = pool.at(pw.page(p8 >> c.lps), p8);
+          kp = c.k + off, vp = c.v + off;
         }
       }
       rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * wave, kd, vd);
@@ -743,11 +763,14 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       if (t < nt) {
         const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
         pw.seek(pos >> c.lps);
-        if (!pw.absent(p16 >> c.lps, 1) && (p16 + 16 > pl.lo || p16 < mask.sink)) valid = bound(pl.hi - p16, 0, 16);
-        row = pool_row(c, pw.page(p16 >> c.lps), h, p16);
-        y.absent = pw.absent(pos >> c.lps, kcols);
+        valid = 16;
+        if (pw.gone != 0 || pos < pl.lo || pos + kWK > pl.hi) {
+          y.absent = pw.absent(pos >> c.lps, kcols);
+          valid = !pw.absent(p16 >> c.lps, 1) && (p16 + 16 > pl.lo || p16 < mask.sink) ? bound(pl.hi - p16, 0, 16) : 0;
+        }
+        row = pool.at(pw.page(p16 >> c.lps), p16);
       }
-      y.x.load((isv ? c.v : c.k) + row * Quarter<FMT, D>::kRow, (isv ? c.vs : c.ks) + row * (D / kGroup), valid, l >> 2, qpart);
+      y.x.load((isv ? c.v : c.k) + row, (isv ? c.vs : c.ks) + row / (Quarter<FMT, D>::kRow / (D / kGroup)), valid, l >> 2, qpart);
     };
     uint32_t absent = 0;
     auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
@@ -1091,14 +1114,17 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
   };
   const int kcols = max(1, kFK >> c.lps);  // pages that a tile lies in
   const Rows8<D> ld = rows8_offsets<D>();
+  const PoolAt pool(c, k.h, FULL ? 2 * D : Quarter<FULL ? DKV_CACHE_FP8 : FMT, D>::kRow);
   // Loads of tile t, always the same number: behind the last tile they read nothing.
   auto issue = [&](int t, char *kd, char *vd) __attribute__((always_inline)) -> uint32_t {
     uint32_t absent = 0;
     const bool isbank = !FULL || t < k.pl.nb, in = t < k.nt;
     const int pos = tile_pos(k.pl, kFK, t);
+    bool edge = false;
     if (in && !isbank) {
       pw.seek(pos >> c.lps);
-      absent = pw.absent(pos >> c.lps, kcols);
+      edge = pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi;
+      if (edge) absent = pw.absent(pos >> c.lps, kcols);
     }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -1111,9 +1137,10 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
           valid = bound(k.pl.m - r8, 0, 8);
         } else {
           const int p8 = pos + 8 * g;
-          if (!pw.absent(p8 >> c.lps, 1) && (p8 + 8 > k.pl.lo || p8 < mask.sink)) valid = bound(k.pl.hi - p8, 0, 8);
-          const size_t row = pool_row(c, pw.page(p8 >> c.lps), k.h, p8);
-          kp = c.k + row * (2 * D), vp = c.v + row * (2 * D);
+          valid = 8;
+          if (edge) valid = !pw.absent(p8 >> c.lps, 1) && (p8 + 8 > k.pl.lo || p8 < mask.sink) ? bound(k.pl.hi - p8, 0, 8) : 0;
+          const size_t off = pool.at(pw.page(p8 >> c.lps), p8);
+          kp = c.k + off, vp = c.v + off;
         }
       }
       rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * g, kd, vd);
@@ -1161,9 +1188,11 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
       const int pos = tile_pos(k.pl, kFK, t);
       const bool in = t < k.nt;
       y.absent = 0;
+      bool edge = false;
       if (in) {
         pw.seek(pos >> c.lps);
-        y.absent = pw.absent(pos >> c.lps, kcols);
+        edge = pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi;
+        if (edge) y.absent = pw.absent(pos >> c.lps, kcols);
       }
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
@@ -1171,11 +1200,14 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
         int valid = 0;
         if (in) {
           const int p16 = pos + 16 * g;
-          if (!pw.absent(p16 >> c.lps, 1) && (p16 + 16 > k.pl.lo || p16 < mask.sink)) valid = bound(k.pl.hi - p16, 0, 16);
-          row = pool_row(c, pw.page(p16 >> c.lps), k.h, p16);
+          valid = 16;
+          if (edge)
+            valid = !pw.absent(p16 >> c.lps, 1) && (p16 + 16 > k.pl.lo || p16 < mask.sink) ? bound(k.pl.hi - p16, 0, 16) : 0;
+          row = pool.at(pw.page(p16 >> c.lps), p16);
         }
-        y.k[g].load(c.k + row * Quarter<FMT, D>::kRow, c.ks + row * (D / kGroup), valid, lr, part4);
-        y.v[g].load(c.v + row * Quarter<FMT, D>::kRow, c.vs + row * (D / kGroup), valid, lr, part4);
+        const size_t srow = row / (Quarter<FMT, D>::kRow / (D / kGroup));  // scales: one byte per group
+        y.k[g].load(c.k + row, c.ks + srow, valid, lr, part4);
+        y.v[g].load(c.v + row, c.vs + srow, valid, lr, part4);
       }
     };
     auto step = [&](auto &y, int t) __attribute__((always_inline)) {

@@ -40,7 +40,9 @@ BAD_CACHES = [
     (dict(page_size=48), -2), (dict(page_size=512), -2), (dict(page_size=0), -2), (dict(num_seqs=0), -2),
     (dict(num_kv_heads=0), -2), (dict(num_pages=0), -2), (dict(max_pages=0), -2),
     (dict(max_pages=(1 << 24) + 1), -2),                                     # more than 2^30 tokens
-    (dict(num_seqs=1 << 20, num_kv_heads=16), -2), (dict(k=None), -1), (dict(v=None), -1), (dict(page_table=None), -1),
+    (dict(num_seqs=1 << 20, num_kv_heads=16), -2),
+    (dict(num_seqs=1, num_kv_heads=1 << 16, page_size=256), -2),              # a page of 2^31 bytes
+    (dict(k=None), -1), (dict(v=None), -1), (dict(page_table=None), -1),
     (dict(length=None), -1), (dict(k_scale=None), -1), (dict(v_scale=None), -1), (dict(k=24), -1), (dict(v=8), -1)]
 
 
@@ -80,7 +82,7 @@ def test_write_and_read_refusals(L):
     assert write(ts=516) == -2 and write(hs=4) == -2    # rows that do not start at 16 bytes
     assert write(ts=514, cache=_cache(api, dtype=1)) == -2
     assert write(T=0, most=0, k=None, v=None) == 0      # nothing to do: nothing is enqueued
-    many = _cache(api, num_seqs=1, num_kv_heads=1 << 20)
+    many = _cache(api, num_seqs=1, num_kv_heads=1 << 19, page_size=16)
     assert write(T=1 << 12, most=1 << 12, cache=many) == -2  # rows of a sequence are 32-bit indices
     assert L.densitykv_cache_read(r(c), None, -1, 16, 16, None) == -2
     assert L.densitykv_cache_read(r(c), None, (1 << 24) + 1, 16, 16, None) == -2
