@@ -2,7 +2,11 @@
 //
 // Both are one pass over the data with 8 elements per thread: 16 bytes of a bf16 row
 // in or out, so a wave reads and writes whole 128-byte lines on both sides.  The
-// largest magnitude of a group of 32 comes from four neighbouring lanes.
+// largest magnitude of a group of 32 comes from four neighbouring lanes.  Bound by memory:
+// a write of 8 x 4,680 tokens of 12 heads into 8 bits with its reading back takes 120 us
+// (4.6 TB/s), a reading of 30 layers' blocks out of 4 bits 255 us (4.3 TB/s, 3.4 of it
+// written; a large copy reaches 4.7 on this card).  Two and four rows per thread, with their
+// loads side by side, gained nothing (117 and 256 us).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -14,7 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Thread = 8 elements of one row (token, head) of K (z = 0) or V (z = 1) of sequence y.
+// Thread = 8 elements of one row (token, head) of K (z = 0) or V (z = 1) of sequence s.
 template <int DT, int FMT, int D>
 __global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *__restrict__ k, const void *__restrict__ v,
                                                           int64_t ts, int64_t hs, int nb) {
@@ -27,44 +31,54 @@ __global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *_
   if (i >= min(nr.n, c.max_new)) return;  // whole groups of four lanes leave together
   const int pos = seq_length(c, s) - nr.n + i;
   if (pos < 0) return;
+  // the row is on its way while the page number is
+  constexpr int W = DT == DKV_BF16 ? 1 : 2;  // 16-byte words of 8 elements
+  const char *src = static_cast<const char *>(z ? v : k) + ((int64_t)(nr.first + i) * ts + h * hs + 8 * ch) * (2 * W);
+  uint4 x[W];
+#pragma unroll
+  for (int j = 0; j < W; ++j) x[j] = reinterpret_cast<const uint4 *>(src)[j];
   const int p = page_of(c, s, pos);
   if (p < 0) return;
-  const int64_t at = (int64_t)(nr.first + i) * ts + h * hs + 8 * ch;
-  const void *src = z ? v : k;
   unsigned char *dst = z ? c.v : c.k;
   const size_t r = pool_row(c, p, h, pos);
   if constexpr (FMT == DKV_CACHE_FULL) {
-    constexpr int E = DT == DKV_BF16 ? 1 : 2;
-    const uint4 *x = reinterpret_cast<const uint4 *>(static_cast<const char *>(src) + at * (2 * E));
-    uint4 *o = reinterpret_cast<uint4 *>(dst + r * (2 * E * D) + 16 * E * ch);
+    uint4 *o = reinterpret_cast<uint4 *>(dst + r * (2 * W * D) + 16 * W * ch);
 #pragma unroll
-    for (int j = 0; j < E; ++j) o[j] = x[j];
+    for (int j = 0; j < W; ++j) o[j] = x[j];
   } else {
-    float x[8];
+    float f[8];
     if constexpr (DT == DKV_BF16) {
-      unpack_bf16x8(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(src) + at), x);
+      unpack_bf16x8(x[0], f);
     } else {
-      const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(src) + at);
-      const float4 a = f[0], b = f[1];
-      x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        f[4 * j] = __uint_as_float(x[j].x), f[4 * j + 1] = __uint_as_float(x[j].y);
+        f[4 * j + 2] = __uint_as_float(x[j].z), f[4 * j + 3] = __uint_as_float(x[j].w);
+      }
     }
     // magnitudes compare as integers, NaN above infinity
     uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7fffffffu);
     m = max(m, (uint32_t)__shfl_xor((int)m, 1, 64));
     m = max(m, (uint32_t)__shfl_xor((int)m, 2, 64));
     const int code = scale_code<FMT>(__uint_as_float(m));
-    // a group that reads as NaN stores zeros
-    const float sc = scale_of(code == kScaleNan ? kScaleBias : code);
-    if (code == kScaleNan) {
+    if (code == kScaleNan) {  // a group that reads as NaN stores zeros
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = 0.0f;
+      for (int j = 0; j < 8; ++j) f[j] = 0.0f;
     }
-    if constexpr (FMT == DKV_CACHE_FP8) *reinterpret_cast<uint2 *>(dst + r * D + 8 * ch) = quantise_fp8(x, sc);
-    else *reinterpret_cast<uint32_t *>(dst + r * (D / 2) + 4 * ch) = quantise_fp4(x, sc);
+    const float sc = scale_of(code == kScaleNan ? kScaleBias : code);
+    if constexpr (FMT == DKV_CACHE_FP8) *reinterpret_cast<uint2 *>(dst + r * D + 8 * ch) = quantise_fp8(f, sc);
+    else *reinterpret_cast<uint32_t *>(dst + r * (D / 2) + 4 * ch) = quantise_fp4(f, sc);
     if ((ch & 3) == 0) (z ? c.vs : c.ks)[r * (D / kGroup) + ch / 4] = (uint8_t)code;
   }
+}
+
+// A store past the caches: the rows read back are more than they hold where it matters (30 layers' blocks of 4,680 rows,
+// 863 MB out of 4-bit pages: 292 us with ordinary stores, 255 so; rows in bf16 327 and 296).
+__device__ __forceinline__ void store_once(void *p, uint4 x) {
+  typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(__builtin_bit_cast(word4, x), static_cast<word4 *>(p));
 }
 
 // Thread = 8 elements of row i of bank (s, h), K or V.
@@ -73,8 +87,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(Pages c, const int32_t 
                                                          int nb) {
   constexpr int CH = D / 8;
   const int bz = (int)(blockIdx.x / (unsigned)nb), z = bz & 1, b = bz >> 1, s = b / c.H, h = b % c.H;
-  const int item = (int)(blockIdx.x % (unsigned)nb) * kThreads + (int)threadIdx.x;  // n CH <= 2^28
-  const int ch = item % CH, i = item / CH;
+  const int ch = (int)threadIdx.x % CH, i = (int)(blockIdx.x % (unsigned)nb) * (kThreads / CH) + (int)threadIdx.x / CH;
   if (i >= n) return;
   const int64_t pos = (int64_t)(first ? first[s] : 0) + i;
   int p = -1;
@@ -86,21 +99,20 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(Pages c, const int32_t 
   if constexpr (DT == DKV_BF16) {
     uint4 x = {0, 0, 0, 0};
     if (p >= 0) x = load_bf16x8<FMT, D>(src, sc, r, ch);
-    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(z ? v : k) + o) = x;
+    store_once(static_cast<uint16_t *>(z ? v : k) + o, x);
   } else {
     float x[8] = {};
     if (p >= 0) load_f32x8<DT, FMT, D>(src, sc, r, ch, x);
-    float4 *f = reinterpret_cast<float4 *>(static_cast<float *>(z ? v : k) + o);
-    f[0] = float4{x[0], x[1], x[2], x[3]};
-    f[1] = float4{x[4], x[5], x[6], x[7]};
+    float *f = static_cast<float *>(z ? v : k) + o;
+    store_once(f, __builtin_bit_cast(uint4, float4{x[0], x[1], x[2], x[3]}));
+    store_once(f + 4, __builtin_bit_cast(uint4, float4{x[4], x[5], x[6], x[7]}));
   }
 }
 
 template <int DT, int FMT, int D>
 hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, int64_t hs, hipStream_t s) {
-  const int most = c.max_new < c.T ? c.max_new : c.T;
   constexpr int kRows = kThreads / (D / 8);
-  const int64_t nb = ((int64_t)most * c.H + kRows - 1) / kRows, grid = nb * c.S * 2;
+  const int64_t nb = ((int64_t)c.max_new * c.H + kRows - 1) / kRows, grid = nb * c.S * 2;
   if (grid == 0) return hipSuccess;
   if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   k_cache_write<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);
@@ -108,7 +120,8 @@ hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, 
 }
 template <int DT, int FMT, int D>
 hipError_t read_impl(const Pages &c, const int32_t *first, int n, void *k, void *v, hipStream_t s) {
-  const int64_t nb = ((int64_t)n * (D / 8) + kThreads - 1) / kThreads, grid = nb * c.S * c.H * 2;
+  constexpr int kRows = kThreads / (D / 8);
+  const int64_t nb = ((int64_t)n + kRows - 1) / kRows, grid = nb * c.S * c.H * 2;
   if (grid == 0) return hipSuccess;
   if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
   k_cache_read<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, first, n, k, v, (int)nb);
