@@ -747,15 +747,16 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       run_direct(tb, t0);
       stage_barrier();
     }
-    // Quantised rows come through registers, two tiles ahead, and are stored as bf16: waves 0-3
+    // Quantised rows come through registers, a tile or two ahead, and are stored as bf16: waves 0-3
     // a quarter row of K per lane, waves 4-7 of V, each wave 16 rows that lie in one page.  Of
     // the two waves of a SIMD one converts before its matrix work and one after it.
     const bool isv = wave >= 4;
     const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
+    constexpr int kAhead = D == 64 ? 2 : 1;  // tiles in registers; two of them do not fit beside 128 columns
     struct {
       Quarter<FMT, D> x;
       uint32_t absent;
-    } f[2];
+    } f[kAhead];
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
       size_t row = 0;
       int valid = 0;
@@ -776,10 +777,12 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
       const uint32_t now = absent, next = y.absent;
       if (!isv) y.x.template store<false>(kn, lr, qpart);
+      asm volatile("" ::: "memory");
+      if (kAhead == 1 && !isv) fetch(y, t + 2);
       if (t < nt) compute(false, t, kt, vt, now);
       if (isv) y.x.template store<true>(vn, lr, qpart);
       asm volatile("" ::: "memory");
-      fetch(y, t + 3);
+      if (kAhead == 2 || isv) fetch(y, t + 1 + kAhead);
       asm volatile("" ::: "memory");
       absent = next;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
@@ -788,18 +791,18 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
     if (t0 < nt) {
       fetch(f[0], t0);
       asm volatile("" ::: "memory");  // the loads in this order, which the waits count on
-      fetch(f[1], t0 + 1);
+      if constexpr (kAhead == 2) fetch(f[kAhead - 1], t0 + 1);
       asm volatile("" ::: "memory");
       if (isv) f[0].x.template store<true>(v0, lr, qpart);
       else f[0].x.template store<false>(k0, lr, qpart);
       absent = f[0].absent;
       asm volatile("" ::: "memory");
-      fetch(f[0], t0 + 2);
+      fetch(f[0], t0 + kAhead);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       stage_barrier();
     }
     for (int t = t0; t < nt; t += 2) {
-      step(t, f[1], k0, v0, k1, v1);
+      step(t, f[kAhead - 1], k0, v0, k1, v1);
       step(t + 1, f[0], k1, v1, k0, v0);
     }
   }
@@ -1177,12 +1180,13 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
       __builtin_amdgcn_s_waitcnt(0xc07f);
       asm volatile("" ::: "memory");
     }
-    // quantised rows through registers, two tiles ahead; a lane: two quarter rows of K and two of
-    // V, in rows l / 4 and 16 + l / 4
+    // quantised rows through registers, two tiles ahead (one where two do not fit the registers); a
+    // lane: two quarter rows of K and two of V, in rows l / 4 and 16 + l / 4
+    constexpr int kAhead = R == 16 || D == 64 ? 2 : 1;
     struct {
       Quarter<FMT, D> k[2], v[2];
       uint32_t absent;
-    } f[2];
+    } f[kAhead];
     const int part4 = l & 3, lr = l >> 2;
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
       const int pos = tile_pos(k.pl, kFK, t);
@@ -1219,7 +1223,7 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
       }
       const uint32_t absent = y.absent;
       asm volatile("" ::: "memory");
-      fetch(y, t + 2 * kFWaves);
+      fetch(y, t + kAhead * kFWaves);
       asm volatile("" ::: "memory");
       __builtin_amdgcn_wave_barrier();
       if (t < k.nt) compute(false, t, ka, va, absent);
@@ -1227,11 +1231,11 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
     };
     fetch(f[0], t);
     asm volatile("" ::: "memory");  // the loads in this order, which the waits count on
-    fetch(f[1], t + kFWaves);
+    if constexpr (kAhead > 1) fetch(f[kAhead - 1], t + kFWaves);
     asm volatile("" ::: "memory");
-    for (; t < k.nt; t += 2 * kFWaves) {
+    for (; t < k.nt; t += kAhead * kFWaves) {
       step(f[0], t);
-      step(f[1], t + kFWaves);
+      if constexpr (kAhead > 1) step(f[kAhead - 1], t + kFWaves);
     }
   }
 
@@ -1469,14 +1473,20 @@ __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankR
 
 constexpr int kCUs = 256;
 constexpr int kMaxSplit = 64;
-constexpr int kFewRows = 64;   // rows of a (sequence, kv head) up to which blocks of 16 or 32 rows are taken
-constexpr int kManySplits = 5; // splits from which a row's partial results are read 8 (16) at a time
+constexpr int kManySplits = 5;  // splits from which a row's partial results are read 8 (d = 64: 16) at a time
+
+// Rows of a (sequence, kv head) up to which blocks of 16 or 32 rows are taken: 64, or 32 where the two stages of bf16
+// rows leave a CU one workgroup (us of 32-row and 256-row blocks, 8 kv heads, up to 8,192 tokens).  8-bit pages, d = 128,
+// 32 sequences: 32 rows 93 and 169, 64 rows 125 and 171, 128 rows 214 and 174; 4 sequences: 28 and 35, 33 and 37, 45 and
+// 44; d = 64, 32 sequences: 64 rows 85 and 135, 128 rows 148 and 137.  bf16 pages, d = 128, 32 sequences: 32 rows 159 and
+// 171, 64 rows 228 and 170.
+int few_rows(int fmt, int d) { return fmt == DKV_CACHE_FULL && d == 128 ? 32 : 64; }
 
 // Rows per row block of a call: 16 or 32 with the keys over the waves, or 256.
-int block_rows(const Pages &c, int dtype, int G) {
+int block_rows(const Pages &c, int dtype, int fmt, int d, int G) {
   const int64_t rows = (int64_t)c.max_new * G;
   if (dtype != DKV_BF16) return 32;
-  return rows <= 16 ? 16 : (rows <= kFewRows ? 32 : kWRows);
+  return rows <= 16 ? 16 : (rows <= few_rows(fmt, d) ? 32 : kWRows);
 }
 
 template <int DT, int D, int RB, int KT, int LEAST>
@@ -1501,7 +1511,7 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
     part.o = static_cast<float *>(ws);
     part.ml = reinterpret_cast<float2 *>(part.o + nrow * nsplit * D);
   }
-  const int R = block_rows(c, DT, qs.G);
+  const int R = block_rows(c, DT, FMT, D, qs.G);
   const int64_t nrb = ((int64_t)c.max_new * qs.G + R - 1) / R;
   const int64_t grid = nrb * c.S * c.H * nsplit;
   if (grid > 0x7fffffffLL || nrow > 0x7fffffffLL) return hipErrorInvalidConfiguration;
@@ -1534,7 +1544,7 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   const int G = nh / c.H;
   const int64_t nrow = (int64_t)c.S * c.max_new * nh;
   if (nrow == 0) return 1;
-  const int RB = block_rows(c, dtype, G);
+  const int RB = block_rows(c, dtype, fmt, d, G);
   const bool few = RB != kWRows;
   const int KT = few ? kFK : kWK, least = few ? kFLeast : kWLeast;
   int64_t keys = (int64_t)c.cols << c.lps;
