@@ -1249,43 +1249,35 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
   join_waves<DKV_BF16, D, R>(k0, v0, wml, k, c, qs, part, qs.scale_log2);
 }
 
-// fp32 scores and products on v_mfma_f32_32x32x2_f32, keys and values straight from memory.
-// K step 4 c + j takes dims 8 c + j and 8 c + 4 + j of both operands.
-template <int FMT, int D>
-__device__ __forceinline__ float4 load_f32x4(const unsigned char *pool, const uint8_t *scale, size_t row, int d0) {
-  if constexpr (FMT == DKV_CACHE_FULL) {
-    return *reinterpret_cast<const float4 *>(pool + row * (4 * D) + 4 * d0);
-  } else {
-    const int code = scale[row * (D / kGroup) + d0 / kGroup];
-    uint32_t lo, hi;
-    if constexpr (FMT == DKV_CACHE_FP8) {
-      const uint4 y = bf16_of_fp8(uint2{*reinterpret_cast<const uint32_t *>(pool + row * D + d0), 0}, code);
-      lo = y.x, hi = y.y;
-    } else {
-      const uint4 y = bf16_of_fp4(*reinterpret_cast<const uint16_t *>(pool + row * (D / 2) + d0 / 2), code);
-      lo = y.x, hi = y.y;
-    }
-    return float4{__uint_as_float(lo << 16), __uint_as_float(lo & 0xffff0000u), __uint_as_float(hi << 16),
-                  __uint_as_float(hi & 0xffff0000u)};
-  }
-}
-template <int FMT, int D>
-__device__ __forceinline__ float load_f32(const unsigned char *pool, const uint8_t *scale, size_t row, int d) {
-  if constexpr (FMT == DKV_CACHE_FULL) {
-    return *reinterpret_cast<const float *>(pool + row * (4 * D) + 4 * d);
-  } else {
-    const int code = scale[row * (D / kGroup) + d / kGroup];
-    uint32_t x;
-    if constexpr (FMT == DKV_CACHE_FP8) x = bf16_of_fp8(uint2{pool[row * D + d], 0}, code).x;
-    else x = bf16_of_fp4(pool[row * (D / 2) + d / 2] >> (4 * (d & 1)), code).x;
-    return __uint_as_float(x << 16);
+// ---------------------------------------------------------------------------
+// fp32: 32 rows per workgroup, the keys over its four waves, scores and products on
+// v_mfma_f32_32x32x2_f32.  Lane (h, n) holds row n; K step 16 kk + j takes the dims 16 kk + j
+// (h = 0) and 16 kk + 8 + j of both operands.  Rows of fp32 go to LDS (keys, a tile ahead) or
+// to registers (values, asked for before the scores); quantised rows are exact in bf16 and go
+// through LDS so.
+// ---------------------------------------------------------------------------
+template <int D>
+__device__ __forceinline__ int kf_swz(int r, int c) { return c ^ (r % 16); }  // 16-byte chunks of a row of 4 D bytes
+
+// 8 rows of fp32 keys into rows r0 .. of a tile, `valid` of them, the others as zeros.
+template <int D>
+__device__ __forceinline__ void rows8_issue_f32(const unsigned char *kp, int valid, int r0, char *kt) {
+  constexpr int CH = D / 4, RPL = 64 / CH, kLoads = 8 / RPL;
+  const int l = threadIdx.x & 63, extent = uni(valid) * (4 * D);
+  const __amdgpu_buffer_rsrc_t rk = __builtin_amdgcn_make_buffer_rsrc((void *)kp, (short)0, extent, kBufferRsrcWord3);
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) {
+    const int r = q * RPL + l / CH, off = r * (4 * D) + 16 * kf_swz<D>(r0 + r, l % CH);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void *)(kt + r0 * (4 * D) + q * 1024), 16, off, 0, 0, 0);
   }
 }
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mask mask, BankRows bank, CacheQueries qs,
                                                                    int nsplit, Part part) {
-  __shared__ __attribute__((aligned(16))) char lo[kFWaves * 64 * D], hi[kFWaves * 64 * D];  // the waves' results at the end
+  constexpr bool FULL = FMT == DKV_CACHE_FULL;
+  constexpr int TB = kFK * 4 * D;  // a tile of fp32 keys; a K and a V tile of bf16
+  __shared__ __attribute__((aligned(1024))) char k0[kFWaves * TB], k1[FULL ? kFWaves * TB : 16];
   __shared__ float2 wml[kFWaves][32];
   __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<32> k;
@@ -1299,102 +1291,263 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mas
   rows.init();
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)k.b * bank.cap * (4 * D);
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)k.b * bank.cap * (4 * D);
-  constexpr int KC = D / 8;
-  float4 qf[KC];
+  char *ka = k0 + wave * TB, *kb = k1 + (FULL ? wave * TB : 0);
+  float qf[D / 16][8];
   {
     const float *q = static_cast<const float *>(qs.q) + at.t * qs.qt + (size_t)at.hq * qs.qh;
 #pragma unroll
-    for (int u = 0; u < KC; ++u) qf[u] = *reinterpret_cast<const float4 *>(q + 8 * u + 4 * lh);
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float4 x = *reinterpret_cast<const float4 *>(q + 16 * kk + 8 * lh + 4 * j);
+        qf[kk][4 * j] = x.x, qf[kk][4 * j + 1] = x.y, qf[kk][4 * j + 2] = x.z, qf[kk][4 * j + 3] = x.w;
+      }
   }
-  auto tile = [&](auto fmt, int t, const unsigned char *kp, const uint8_t *ks, const unsigned char *vp, const uint8_t *vs,
-                  auto row_of, uint32_t okbits) __attribute__((always_inline)) {
-    // okbits: rows of the tile that may be read; the others count as zeros
-    constexpr int F = decltype(fmt)::value;
+  const int kcols = max(1, kFK >> c.lps);
+  const PoolAt pool(c, k.h, FULL ? 4 * D : Quarter<FULL ? DKV_CACHE_FP8 : FMT, D>::kRow);
+
+  // The 8-row groups of a tile of fp32 rows: where they are and how many rows of each may be read (none behind the
+  // last tile).
+  struct Groups {
+    const unsigned char *kp[4], *vp[4];
+    int valid[4];
+    uint32_t absent;
+  };
+  auto groups_of = [&](int t) __attribute__((always_inline)) {
+    Groups g;
+    g.absent = 0;
+    const bool isbank = !FULL || t < k.pl.nb, in = t < k.nt;
     const int pos = tile_pos(k.pl, kFK, t);
-    const bool kok = (okbits >> n) & 1;
-    const size_t krow = row_of(n);
-    // the values are on their way while the scores are computed
-    float vx[D / 32][16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i >> 2) + 4 * lh + (i & 3);
-      const bool ok = (okbits >> key) & 1;
-      const size_t vrow = row_of(key);
-#pragma unroll
-      for (int t2 = 0; t2 < D / 32; ++t2) vx[t2][i] = ok ? load_f32<F, D>(vp, vs, vrow, 32 * t2 + n) : 0.0f;
+    bool edge = false;
+    if (in && !isbank) {
+      pw.seek(pos >> c.lps);
+      edge = pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi;
+      if (edge) g.absent = pw.absent(pos >> c.lps, kcols);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      size_t off = 0;
+      g.valid[j] = 0;
+      if (in && isbank) {
+        const int r8 = t * kFK + 8 * j;
+        off = (size_t)r8 * (4 * D);
+        g.valid[j] = uni(bound(k.pl.m - r8, 0, 8));
+      } else if (in) {
+        const int p8 = pos + 8 * j;
+        g.valid[j] = 8;
+        if (edge)
+          g.valid[j] = uni(!pw.absent(p8 >> c.lps, 1) && (p8 + 8 > k.pl.lo || p8 < mask.sink) ? bound(k.pl.hi - p8, 0, 8) : 0);
+        off = pool.at(pw.page(p8 >> c.lps), p8);
+      }
+      g.kp[j] = (isbank ? bk : c.k) + off;
+      g.vp[j] = (isbank ? bv : c.v) + off;
+    }
+    return g;
+  };
+  auto issue_keys = [&](const Groups &g, char *kt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) rows8_issue_f32<D>(g.kp[j], g.valid[j], 8 * j, kt);
+  };
+  // Value register i of column tile t2: key 8 (i / 4) + 4 h + i % 4, element 32 t2 + n.
+  auto load_values = [&](const Groups &g, float (*vx)[16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __amdgpu_buffer_rsrc_t rv =
+          __builtin_amdgcn_make_buffer_rsrc((void *)g.vp[j], (short)0, g.valid[j] * (4 * D), kBufferRsrcWord3);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int t2 = 0; t2 < D / 32; ++t2)
+          vx[t2][4 * j + e] = __uint_as_float(
+              __builtin_amdgcn_raw_buffer_load_b32(rv, (4 * lh + e) * (4 * D) + 4 * n + 128 * t2, 0, 0));
+    }
+  };
+  auto scores_f32 = [&](const char *kt) __attribute__((always_inline)) {
     f32x16 sc = {};
 #pragma unroll
-    for (int u = 0; u < KC; ++u) {
-      float4 kx = {0, 0, 0, 0};
-      if (kok) kx = load_f32x4<F, D>(kp, ks, krow, 8 * u + 4 * lh);
-      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.x, qf[u].x, sc, 0, 0, 0);
-      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.y, qf[u].y, sc, 0, 0, 0);
-      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.z, qf[u].z, sc, 0, 0, 0);
-      sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kx.w, qf[u].w, sc, 0, 0, 0);
+    for (int kk = 0; kk < D / 16; ++kk)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float4 x = *reinterpret_cast<const float4 *>(kt + n * (4 * D) + 16 * kf_swz<D>(n, 4 * kk + 2 * lh + j));
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.x, qf[kk][4 * j], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.y, qf[kk][4 * j + 1], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.z, qf[kk][4 * j + 2], sc, 0, 0, 0);
+        sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x.w, qf[kk][4 * j + 3], sc, 0, 0, 0);
+      }
+    return sc;
+  };
+  // Softmax update and products of a tile; not `whole`: only the keys of vis.
+  auto finish = [&](f32x16 sc, float (*vx)[16], int nvalid, bool whole, uint32_t vis) __attribute__((always_inline)) {
+    if (whole) {
+      rows.any = true;
+      vis = ~0u;
+    } else {
+      rows.any |= (vis & 0x0f0f0f0fu) != 0;
     }
-    uint32_t vis = 0;
     float tmax = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i >> 2) + 4 * lh + (i & 3);
-      const bool ok = ((okbits >> key) & 1) && (t < k.pl.nb || sees(wm.row, wm.sink, pos + key));
-      if (ok) vis |= 1u << i;
-      sc[i] = ok ? sc[i] * qs.scale_log2 : -INFINITY;
+      const int key = 8 * (i >> 2) + (i & 3);
+      sc[i] = ((vis >> key) & 1) && key + 4 * lh < nvalid ? sc[i] * qs.scale_log2 : -INFINITY;
       tmax = fmaxf(tmax, sc[i]);
     }
-    rows.any |= vis != 0;
     tmax = fmaxf(tmax, __shfl_xor(tmax, 32, 64));
     const float mnew = fmaxf(rows.mrun, tmax);
-    const float mref = mnew == -INFINITY ? 0.0f : mnew;
+    const float mref = mnew == -INFINITY ? 0.0f : mnew;  // scores of -inf alone: weights 0, not inf - inf
     const float corr = exp2f(rows.mrun - mref);
     rows.mrun = mnew;
-    float pw_[16], ps = 0.0f;
+    float w[16], ps = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      pw_[i] = exp2f(sc[i] - mref);
-      ps += pw_[i];
+      w[i] = exp2f(sc[i] - mref);
+      ps += w[i];
     }
     rows.lrun = __builtin_fmaf(rows.lrun, corr, ps);
 #pragma unroll
-    for (int t2 = 0; t2 < D / 32; ++t2) {
-      bool bad = false;
+    for (int t2 = 0; t2 < D / 32; ++t2) rows.o[t2] *= corr;
+    if (!whole) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) bad |= (__float_as_uint(vx[t2][i]) & 0x7f800000u) == 0x7f800000u;
-      rows.o[t2] *= corr;
-      if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it
-        f32x16 kinds = {};
+      for (int t2 = 0; t2 < D / 32; ++t2) {
+        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t u = __float_as_uint(vx[t2][i]);
-          const float kind = (u & 0x7fffffffu) < 0x7f800000u ? 0.0f : ((u & 0x7fffffffu) > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
-          kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> i) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
-          if (kind != 0.0f) vx[t2][i] = 0.0f;
+        for (int i = 0; i < 16; ++i) bad |= (__float_as_uint(vx[t2][i]) & 0x7f800000u) == 0x7f800000u;
+        if (__any(bad)) {  // not finite: out of the product, and added to the rows that see it (see purge)
+          f32x16 kinds = {};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t u = __float_as_uint(vx[t2][i]);
+            const uint32_t m = u & 0x7fffffffu;
+            const float kind = m < 0x7f800000u ? 0.0f : (m > 0x7f800000u ? 16384.0f : (u >> 31 ? 128.0f : 1.0f));
+            kinds = __builtin_amdgcn_mfma_f32_32x32x2f32(kind, (vis >> (8 * (i >> 2) + (i & 3))) & 1 ? 1.0f : 0.0f, kinds, 0, 0, 0);
+            if (kind != 0.0f) vx[t2][i] = 0.0f;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
         }
+      }
+    }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) rows.o[t2][i] += value_of_kinds(kinds[i]);
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int t2 = 0; t2 < D / 32; ++t2)
+        rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[t2][i], w[i], rows.o[t2], 0, 0, 0);
+  };
+  auto visible = [&](int t, uint32_t absent, bool &whole) __attribute__((always_inline)) {
+    const int pos = tile_pos(k.pl, kFK, t);
+    whole = absent == 0 && wm.all(pos, kFK);
+    return whole ? 0u : visible_bits(wm, pos, 0, absent, c.lps, lh);
+  };
+
+  if constexpr (FULL) {
+    // keys two stages: a tile in flight while the other is used
+    constexpr int kLoads = D / 8, kYounger = 16 * (D / 32) + kLoads;  // a tile's key loads; and its values before the next keys
+    Groups g = groups_of(k.tb + wave);
+    issue_keys(g, ka);
+    auto step = [&](int t, const char *kt, char *kn) __attribute__((always_inline)) {
+      float vx[D / 32][16];
+      load_values(g, vx);
+      asm volatile("" ::: "memory");
+      const uint32_t absent = g.absent;
+      g = groups_of(t + kFWaves);
+      issue_keys(g, kn);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kYounger < 63 ? kYounger : 63));  // this tile's keys are there
+      asm volatile("" ::: "memory");
+      if (t < k.nt) {
+        const bool isbank = t < k.pl.nb;
+        bool whole = true;
+        uint32_t vis = 0;
+        if (!isbank) vis = visible(t, absent, whole);
+        finish(scores_f32(kt), vx, isbank ? k.pl.m - t * kFK : kFK, whole, vis);
+      }
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // its reads are done before the stage is loaded again
+      asm volatile("" ::: "memory");
+    };
+    for (int t = k.tb + wave; t < k.nt; t += 2 * kFWaves) {
+      step(t, ka, kb);
+      step(t + kFWaves, kb, ka);
+    }
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));  // nothing is on its way to the stages
+  } else {
+    int t = k.tb + wave;
+    for (; t < min(k.nt, k.pl.nb); t += kFWaves) {
+      const Groups g = groups_of(t);
+      float vx[D / 32][16];
+      issue_keys(g, ka);
+      load_values(g, vx);
+      __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
+      asm volatile("" ::: "memory");
+      finish(scores_f32(ka), vx, k.pl.m - t * kFK, true, 0);
+      __builtin_amdgcn_s_waitcnt(0xc07f);
+      asm volatile("" ::: "memory");
+    }
+    // quantised rows as in the bf16 kernel, one tile ahead; the tile is read as floats
+    char *va = ka + TB / 2;
+    Quarter<FMT, D> xk[2], xv[2];
+    const int part4 = l & 3, lr = l >> 2;
+    uint32_t ahead = 0;
+    auto fetch = [&](int t2) __attribute__((always_inline)) {
+      const int pos = tile_pos(k.pl, kFK, t2);
+      const bool in = t2 < k.nt;
+      bool edge = false;
+      ahead = 0;
+      if (in) {
+        pw.seek(pos >> c.lps);
+        edge = pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi;
+        if (edge) ahead = pw.absent(pos >> c.lps, kcols);
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) rows.o[t2] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[t2][i], pw_[i], rows.o[t2], 0, 0, 0);
+      for (int g = 0; g < 2; ++g) {
+        size_t row = 0;
+        int valid = 0;
+        if (in) {
+          const int p16 = pos + 16 * g;
+          valid = 16;
+          if (edge)
+            valid = !pw.absent(p16 >> c.lps, 1) && (p16 + 16 > k.pl.lo || p16 < mask.sink) ? bound(k.pl.hi - p16, 0, 16) : 0;
+          row = pool.at(pw.page(p16 >> c.lps), p16);
+        }
+        const size_t srow = row / (Quarter<FMT, D>::kRow / (D / kGroup));
+        xk[g].load(c.k + row, c.ks + srow, valid, lr, part4);
+        xv[g].load(c.v + row, c.vs + srow, valid, lr, part4);
+      }
+    };
+    fetch(t);
+    for (; t < k.nt; t += kFWaves) {
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        xk[g].template store<false>(ka, 16 * g + lr, part4);
+        xv[g].template store<true>(va, 16 * g + lr, part4);
+      }
+      const uint32_t absent = ahead;
+      asm volatile("" ::: "memory");
+      fetch(t + kFWaves);
+      asm volatile("" ::: "memory");
+      f32x16 sc = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        float x[8];
+        unpack_bf16x8(*reinterpret_cast<const uint4 *>(ka + n * (2 * D) + 16 * k_swz<D>(n, 2 * kk + lh)), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[j], qf[kk][j], sc, 0, 0, 0);
+      }
+      float vx[D / 32][16];
+#pragma unroll
+      for (int t2 = 0; t2 < D / 32; ++t2)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = 8 * (i >> 2) + 4 * lh + (i & 3), col = 32 * t2 + n;
+          vx[t2][i] = __uint_as_float(
+              (uint32_t)*reinterpret_cast<const uint16_t *>(va + key * (2 * D) + 16 * v_swz<D>(key, col >> 3) + 2 * (col & 7)) << 16);
+        }
+      bool whole;
+      const uint32_t vis = visible(t, absent, whole);
+      finish(sc, vx, kFK, whole, vis);
+      asm volatile("" ::: "memory");
     }
-  };
-  for (int t = k.tb + wave; t < k.nt; t += kFWaves) {
-    if (t < k.pl.nb) {
-      const int nv = min(kFK, k.pl.m - t * kFK);
-      tile(std::integral_constant<int, DKV_CACHE_FULL>(), t, bk, nullptr, bv, nullptr,
-           [&](int key) { return (size_t)t * kFK + key; }, nv >= 32 ? 0xffffffffu : (1u << nv) - 1u);
-      continue;
-    }
-    const int pos = tile_pos(k.pl, kFK, t);
-    pw.seek(pos >> c.lps);
-    const int pa = pw.page(pos >> c.lps), pb = pw.page((pos + 16) >> c.lps);
-    uint32_t okbits = (pw.absent(pos >> c.lps, 1) ? 0u : 0xffffu) | (pw.absent((pos + 16) >> c.lps, 1) ? 0u : 0xffff0000u);
-    if (k.pl.hi - pos < 32) okbits &= (1u << (k.pl.hi - pos)) - 1u;
-    // rows before the window of every row block's token and behind the first tokens are not read
-    tile(std::integral_constant<int, FMT>(), t, c.k, c.ks, c.v, c.vs,
-         [&](int key) { return pool_row(c, key < 16 ? pa : pb, k.h, pos + key); }, okbits);
   }
 
+  __syncthreads();  // the results go where other waves had their tiles
+  char *lo = k0, *hi = k0 + kFWaves * 64 * D;
   if (n < k.here) {
     float *mo = reinterpret_cast<float *>(n < 16 ? lo : hi) + (16 * wave + n % 16) * D;
     const float2 ml = rows.stats();
