@@ -388,8 +388,10 @@ typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_ca
  *   length           [S] int32   tokens of each sequence, the new ones of a chunk
  *                    included; clamped on the device to [0, max_pages * page_size]
  * Rows at or behind the length, and pages that no visible token lies in, may hold
- * anything.  A page may belong to several sequences as long as no call writes to
- * it for more than one of them.
+ * anything.  A page may be in several entries of the table as long as no call
+ * writes to it through more than one of them.
+ * The (token, head) rows of a call, S * max_new of them per head, are limited to
+ * 2^31 - 1024 (DKV_ERR_SHAPE).
  */
 typedef struct {
   int32_t num_seqs;     /* S >= 1 */
@@ -451,7 +453,7 @@ int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n
  *              0: all of them
  */
 typedef struct {
-  int32_t num_heads; /* a multiple of num_kv_heads, T * num_heads < 2^31 */
+  int32_t num_heads; /* a multiple of num_kv_heads, less than 2^20 */
   int32_t window;    /* 0..2^30 */
   int32_t n_sink;    /* 0..2^30 */
   int32_t causal;

@@ -183,6 +183,9 @@ Geom geom_of(const dkv_bank *bk, int n) {
 
 bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
+// Rows (token, head) of a call over the cache: 32-bit numbers in the kernels, with room for rounding up to a row block.
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1024;
+
 int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   if (!c) return DKV_ERR_INVALID;
   if (c->dtype != DKV_BF16 && c->dtype != DKV_F32) return DKV_ERR_INVALID;
@@ -210,7 +213,7 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   out->start = ch->start;
   out->T = ch->n_tokens;
   out->max_new = ch->max_new < ch->n_tokens ? ch->max_new : ch->n_tokens;
-  if ((int64_t)out->max_new * c->num_kv_heads >= (int64_t(1) << 31)) return DKV_ERR_SHAPE;
+  if ((int64_t)out->max_new * c->num_kv_heads * c->num_seqs >= kMaxRows) return DKV_ERR_SHAPE;
   return DKV_OK;
 }
 
@@ -236,7 +239,9 @@ int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dk
     *rows = BankRows{bank->k, bank->v, bank->occupancy, bank->budget, bank->capacity};
   }
   if (qs->num_heads < 1 || qs->num_heads % c->H != 0) return DKV_ERR_SHAPE;
-  if ((int64_t)c->T * qs->num_heads >= (int64_t(1) << 31)) return DKV_ERR_SHAPE;
+  if (qs->num_heads >= (1 << 20) || (int64_t)c->T * qs->num_heads >= kMaxRows ||
+      (int64_t)c->S * c->max_new * qs->num_heads >= kMaxRows)
+    return DKV_ERR_SHAPE;
   constexpr int32_t kMax = 1 << 30;
   if (qs->window < 0 || qs->window > kMax || qs->n_sink < 0 || qs->n_sink > kMax) return DKV_ERR_SHAPE;
   if (!(qs->softmax_scale > 0.0f) || qs->softmax_scale > 1e6f) return DKV_ERR_RANGE;
@@ -416,7 +421,7 @@ int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n
   Pages c{};
   int rc = check_cache(cache, nullptr, &c);
   if (rc) return rc;
-  if (n < 0 || n > (1 << 24)) return DKV_ERR_SHAPE;
+  if (n < 0 || n > (1 << 24) || (int64_t)n * c.S * c.H >= kMaxRows) return DKV_ERR_SHAPE;
   if (n > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
   hipError_t e = launch_cache_read(c, cache->dtype, cache->format, cache->head_dim, first, n, k, v,
                                    static_cast<hipStream_t>(stream));

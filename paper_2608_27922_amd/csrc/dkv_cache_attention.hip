@@ -149,6 +149,7 @@ struct PageWindow {
   const int32_t *row;
   int *next;      // 64 entries, of this wave
   int cols, P, base, cur;
+  int tiles;      // since the numbers were loaded, the present one included
   uint64_t gone;  // bit i: column base + i is absent
   __device__ __forceinline__ int clamped(int c0) const {  // columns past the table repeat its last one: never asked for
     return min(c0 + (int)(threadIdx.x & 63), cols - 1);
@@ -160,14 +161,17 @@ struct PageWindow {
     next = lds;
     base = -256;
     cur = 0;
+    tiles = 0;
     gone = 0;
   }
-  // Columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page).  Tiles ascend
-  // by at most 8 columns, so at least 16 loads of tiles have been issued after the load of `next` when it is needed:
-  // all but the 16 youngest loads being done, it is there, and the tiles on their way are not waited for.
+  // Columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page); one call for
+  // each tile, followed by its loads, two of them at least.  After eight tiles at least 16 loads are younger than that of
+  // `next`: all but the 16 youngest being done, it is there, and the tiles on their way are not waited for.  Earlier (the
+  // window may begin soon behind the first tokens) the numbers are loaded again.
   __device__ __forceinline__ void seek(int col) {
+    ++tiles;
     if (col >= base && col < base + 64) return;
-    if (col >= base + 64 && col < base + 128) {
+    if (col >= base + 64 && col < base + 128 && tiles > 8) {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(16));
       asm volatile("" ::: "memory");
       cur = ((const __attribute__((address_space(3))) int *)next)[threadIdx.x & 63];
@@ -178,6 +182,7 @@ struct PageWindow {
       cur = row[clamped(base)];
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(0));
     }
+    tiles = 1;
     asm volatile("" ::: "memory");
     gone = __ballot((unsigned)cur >= (unsigned)P);  // the numbers come from the caller's array and are bounded here
     if ((unsigned)cur >= (unsigned)P) cur = 0;

@@ -86,6 +86,7 @@ def test_write_and_read_refusals(L):
     assert write(T=1 << 12, most=1 << 12, cache=many) == -2  # rows of a sequence are 32-bit indices
     assert L.densitykv_cache_read(r(c), None, -1, 16, 16, None) == -2
     assert L.densitykv_cache_read(r(c), None, (1 << 24) + 1, 16, 16, None) == -2
+    assert L.densitykv_cache_read(r(_cache(api, num_seqs=64)), None, 1 << 24, 16, 16, None) == -2  # 2^32 rows
     assert L.densitykv_cache_read(r(c), None, 4, None, 16, None) == -1
     assert L.densitykv_cache_read(r(c), None, 4, 16, 8, None) == -1
     assert L.densitykv_cache_read(r(c), None, 0, None, None, None) == 0
@@ -102,7 +103,8 @@ def test_attention_refusals(L):
 
     assert attend(num_heads=0) == -2 and attend(num_heads=6) == -2
     assert attend(window=-1) == -2 and attend(n_sink=-1) == -2 and attend(window=(1 << 30) + 1) == -2
-    assert attend(T=1 << 24, num_heads=128) == -2
+    assert attend(T=1 << 24, num_heads=128) == -2 and attend(num_heads=1 << 20) == -2
+    assert attend(T=1 << 20, most=1 << 20, num_heads=1024) == -2   # 2 sequences x 2^20 x 1024 rows
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert attend(softmax_scale=scale) == -5
     assert attend(q=None) == -1 and attend(out=None) == -1 and attend(q=24) == -1 and attend(out=24) == -1

@@ -302,6 +302,20 @@ def test_attention_pages_and_windows(page, fmt):
         s.check([40, 1, 77], 2, window=window, n_sink=sink, causal=False)
 
 
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", "full", 64), ("bf16", "fp8", 128), ("bf16", "fp4", 64), ("f32", "full", 64),
+                                         ("f32", "fp8", 64)])
+@pytest.mark.parametrize("new", ([1, 1], [90, 20]))
+def test_attention_windows_that_begin_far_behind_the_first_tokens(dtype, fmt, d, new):
+    """From the first tokens the walk goes on at a page 64 to 127 columns later, after one tile or a few, and on from
+    there over more than 64 columns."""
+    s = Setup([2400, 1900], 1, d, 16, fmt, dtype, seed=11)
+    first = 2400 - new[0]
+    for column in (64, 65, 100, 127):
+        for sink in (1, 64, 200):
+            s.check(new, 1, window=first - 16 * column + 1, n_sink=sink)
+    s.check(new, 1, window=2400 - 16 * 64, n_sink=16, causal=False, bank=s.bank(70, [70, 33]))
+
+
 @pytest.mark.parametrize("dtype,fmt", [("bf16", "full"), ("bf16", "fp8"), ("bf16", "fp4"), ("f32", "full"), ("f32", "fp4")])
 def test_attention_of_many_rows(dtype, fmt):
     """Chunks of several row blocks, heads in groups, bank banks of uneven occupancy (one empty)."""
@@ -515,6 +529,54 @@ def test_captured_steps_replay_on_new_contents(fmt, dtype):
         for a, b in zip(pools(s.cache), pools(ref.cache)):
             assert torch.equal(a.nan_to_num(3.0) if a.is_floating_point() else a,
                                b.nan_to_num(3.0) if b.is_floating_point() else b)
+
+
+def test_captured_without_a_workspace_of_its_own():
+    """A split call captured with the partial results in the graph's own memory, replayed among other work."""
+    s = Setup([5000, 3000], 2, 128, 64, "fp8", seed=2)
+    q, start = s.queries([1, 1], 4)
+    size = api.cache_attention(s.cache, q, start, max_new=1)      # the library is loaded before the capture
+    want = size.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = api.cache_attention(s.cache, q, start, max_new=1)
+    for _ in range(4):
+        junk = [torch.full((1 << 20,), 3.0, device="cuda") for _ in range(4)]
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        del junk
+
+
+@pytest.mark.parametrize("fmt,dtype", [("full", "bf16"), ("fp4", "bf16"), ("fp8", "f32")])
+def test_two_calls_at_once(fmt, dtype):
+    """Calls on two streams, each with partial results of its own, among them one that writes other pages."""
+    a, b = Setup([6000, 3000], 2, 128, 16, fmt, dtype, seed=1), Setup([4000, 5000], 2, 128, 32, fmt, dtype, seed=2)
+    (qa, start), (qb, _) = a.queries([1, 1], 4), b.queries([1, 1], 4)
+    wa, wb = (api.cache_attention(x.cache, q, start, max_new=1) for x, q in ((a, qa), (b, qb)))
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(6):
+        for i, (x, q) in enumerate(((a, qa), (b, qb))):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(api.cache_attention(x.cache, q, start, max_new=1))
+    torch.cuda.synchronize()
+    assert all(torch.equal(t, wa) for t in got[0]) and all(torch.equal(t, wb) for t in got[1])
+
+
+@pytest.mark.parametrize("S", (1, 63, 64, 65, 200))
+def test_many_sequences_of_uneven_chunks(S):
+    """Row blocks are found over more sequences than a wave has lanes, many of them without new tokens."""
+    rng = np.random.default_rng(S)
+    lengths = [int(x) for x in rng.integers(0, 40, S)]
+    s = Setup(lengths, 1, 64, 16, "fp8", seed=S, cols=3)
+    for most in (1, 3, 40):
+        new = [int(min(n, x)) for n, x in zip(lengths, rng.integers(0, most + 1, S))]
+        new[-1] = min(lengths[-1], most)
+        if max(new) > 0:
+            s.check(new, 3, pad=2)
 
 
 def test_offsets_beyond_32_bits():
