@@ -381,7 +381,7 @@ typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_ca
 
 /*
  *   k, v             [P, H, page_size, row bytes]   16-byte aligned
- *   k_scale, v_scale [P, H, page_size, d / 32]      NULL for DKV_CACHE_FULL
+ *   k_scale, v_scale [P, H, page_size, d / 32]      4-byte aligned; NULL for DKV_CACHE_FULL
  *   page_table       [S, max_pages] int32           page of the tokens page_size i ..
  *                    of a sequence; an entry outside [0, P) is an absent page: its
  *                    tokens are not written, read as zeros and are not attended
@@ -391,7 +391,8 @@ typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_ca
  * anything.  A page may be in several entries of the table as long as no call
  * writes to it through more than one of them.
  * The (token, head) rows of a call, S * max_new of them per head, are limited to
- * 2^31 - 1024 (DKV_ERR_SHAPE).
+ * 2^31 - 1024, and what a call writes or reads back to about 2^35 elements of K and
+ * V together (its launch has less than 2^32 threads): DKV_ERR_SHAPE otherwise.
  */
 typedef struct {
   int32_t num_seqs;     /* S >= 1 */

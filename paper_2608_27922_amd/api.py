@@ -557,8 +557,9 @@ def cache_attention(cache: PagedCache, q: torch.Tensor, start: Optional[torch.Te
     up to its own position, of those the last `window` (0: all) and the first `n_sink`.  The partial results of a split call
     are in `workspace` (on the cache's device) if it is given, else in a buffer of the caching allocator, held for the call."""
     shape, st, pq = _check_rows(cache, q, "q")
-    if out is None:  # a ragged chunk may leave rows without a sequence
-        out = (torch.zeros if start is not None else torch.empty)(shape, dtype=q.dtype, device=q.device)
+    if out is None:  # a ragged chunk may leave rows without a sequence, a max_new below the longest its last ones
+        whole = start is None and max_new is None
+        out = (torch.empty if whole else torch.zeros)(shape, dtype=q.dtype, device=q.device)
     oshape, ost, po = _check_rows(cache, out, "out")
     if oshape != shape:
         raise ValueError("out must have the shape of q")

@@ -204,6 +204,8 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   if (!c->k || !c->v || !c->page_table || !c->length) return DKV_ERR_INVALID;
   if (c->format != DKV_CACHE_FULL && (!c->k_scale || !c->v_scale)) return DKV_ERR_INVALID;
   if (!aligned16(c->k) || !aligned16(c->v)) return DKV_ERR_INVALID;
+  if (c->format != DKV_CACHE_FULL && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3))
+    return DKV_ERR_INVALID;
   *out = Pages{static_cast<unsigned char *>(c->k), static_cast<unsigned char *>(c->v), c->k_scale, c->v_scale,
                c->page_table, c->length, nullptr, c->num_seqs, c->num_kv_heads, c->num_pages, c->max_pages, lps, 0, 0};
   if (!ch) return DKV_OK;
@@ -215,6 +217,11 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   out->max_new = ch->max_new < ch->n_tokens ? ch->max_new : ch->n_tokens;
   if ((int64_t)out->max_new * c->num_kv_heads * c->num_seqs >= kMaxRows) return DKV_ERR_SHAPE;
   return DKV_OK;
+}
+
+// Status of a launcher of the cache's kernels, which refuses a grid that is too large before it enqueues anything.
+int cache_status(hipError_t e) {
+  return e == hipSuccess ? DKV_OK : (e == hipErrorInvalidConfiguration ? DKV_ERR_SHAPE : DKV_ERR_HIP);
 }
 
 // Strides of rows that are read 16 bytes at a time.
@@ -414,7 +421,7 @@ int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const 
   if (c.max_new > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
   hipError_t e = launch_cache_write(c, cache->dtype, cache->format, cache->head_dim, k, v, token_stride, head_stride,
                                     static_cast<hipStream_t>(stream));
-  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
+  return cache_status(e);
 }
 
 int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n, void *k, void *v, void *stream) {
@@ -425,7 +432,7 @@ int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n
   if (n > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
   hipError_t e = launch_cache_read(c, cache->dtype, cache->format, cache->head_dim, first, n, k, v,
                                    static_cast<hipStream_t>(stream));
-  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
+  return cache_status(e);
 }
 
 int densitykv_cache_attention_workspace_size(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank,
@@ -457,7 +464,7 @@ int densitykv_cache_attention(const dkv_cache *cache, const dkv_chunk *chunk, co
                         qs->num_heads, qs->num_heads / c.H, qs->softmax_scale * 1.4426950408889634f};
   hipError_t e = launch_cache_attention(c, cache->dtype, cache->format, cache->head_dim, mask, rows, cq, workspace, nsplit,
                                         static_cast<hipStream_t>(stream));
-  return e == hipSuccess ? DKV_OK : DKV_ERR_HIP;
+  return cache_status(e);
 }
 
 int densitykv_pair_weight_q23(const float *d2, int64_t n, const dkv_params *prm, int32_t *w_q23,

@@ -114,7 +114,7 @@ hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, 
   constexpr int kRows = kThreads / (D / 8);
   const int64_t nb = ((int64_t)c.max_new * c.H + kRows - 1) / kRows, grid = nb * c.S * 2;
   if (grid == 0) return hipSuccess;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (!grid_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   k_cache_write<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);
   return hipGetLastError();
 }
@@ -123,7 +123,7 @@ hipError_t read_impl(const Pages &c, const int32_t *first, int n, void *k, void 
   constexpr int kRows = kThreads / (D / 8);
   const int64_t nb = ((int64_t)n + kRows - 1) / kRows, grid = nb * c.S * c.H * 2;
   if (grid == 0) return hipSuccess;
-  if (grid > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (!grid_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   k_cache_read<DT, FMT, D><<<(unsigned)grid, kThreads, 0, s>>>(c, first, n, k, v, (int)nb);
   return hipGetLastError();
 }

@@ -1672,7 +1672,7 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
   const int R = block_rows(c, DT, FMT, D, qs.G);
   const int64_t nrb = ((int64_t)c.max_new * qs.G + R - 1) / R;
   const int64_t grid = nrb * c.S * c.H * nsplit;
-  if (grid > 0x7fffffffLL || nrow > 0x7fffffffLL) return hipErrorInvalidConfiguration;
+  if (!grid_fits(grid, 64 * kWWaves) || (nsplit > 1 && !grid_fits(nrow, 256))) return hipErrorInvalidConfiguration;
   const unsigned g = (unsigned)grid;
   if constexpr (DT == DKV_BF16) {
     if (R == kWRows) {

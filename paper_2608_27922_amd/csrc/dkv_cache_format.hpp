@@ -9,8 +9,6 @@
 
 namespace dkv {
 
-typedef float cf32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 cbf16x2 __attribute__((ext_vector_type(2)));
 typedef short cs16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kGroup = 32;          // elements per scale
@@ -18,10 +16,8 @@ constexpr int kScaleBias = 127;
 constexpr int kScaleFirst = -100;   // smallest exponent written: no value of a group is subnormal in bf16
 constexpr int kScaleNan = 255;      // group that held a NaN or an infinity
 
-// Bytes of a row of D elements.
-__host__ __device__ constexpr int row_bytes(int fmt, int dtype, int D) {
-  return fmt == DKV_CACHE_FULL ? D * (dtype == DKV_BF16 ? 2 : 4) : (fmt == DKV_CACHE_FP8 ? D : D / 2);
-}
+// A launch has less than 2^32 threads.
+inline bool grid_fits(int64_t workgroups, int threads) { return workgroups <= 0xffffffffLL / threads; }
 
 // Scale code of a group whose largest magnitude is amax: the smallest exponent e with
 // amax <= F 2^e.  F = 1.75 * 2^8 (e4m3) or 1.5 * 2^2 (e2m1), so with amax = 1.f * 2^a

@@ -24,7 +24,7 @@ def L():
 
 def _cache(api, **kw):
     f = dict(num_seqs=2, num_kv_heads=4, head_dim=128, page_size=64, num_pages=10, max_pages=5, dtype=0, format=1, k=16,
-             v=32, k_scale=1, v_scale=1, page_table=4, length=4)
+             v=32, k_scale=4, v_scale=8, page_table=4, length=4)
     f.update(kw)
     return api.DkvCache(*f.values())
 
@@ -43,7 +43,8 @@ BAD_CACHES = [
     (dict(num_seqs=1 << 20, num_kv_heads=16), -2),
     (dict(num_seqs=1, num_kv_heads=1 << 16, page_size=256), -2),              # a page of 2^31 bytes
     (dict(k=None), -1), (dict(v=None), -1), (dict(page_table=None), -1),
-    (dict(length=None), -1), (dict(k_scale=None), -1), (dict(v_scale=None), -1), (dict(k=24), -1), (dict(v=8), -1)]
+    (dict(length=None), -1), (dict(k_scale=None), -1), (dict(v_scale=None), -1), (dict(k=24), -1), (dict(v=8), -1),
+    (dict(k_scale=6), -1), (dict(v_scale=1), -1)]
 
 
 @pytest.mark.parametrize("kw,code", BAD_CACHES)
@@ -87,6 +88,8 @@ def test_write_and_read_refusals(L):
     assert L.densitykv_cache_read(r(c), None, -1, 16, 16, None) == -2
     assert L.densitykv_cache_read(r(c), None, (1 << 24) + 1, 16, 16, None) == -2
     assert L.densitykv_cache_read(r(_cache(api, num_seqs=64)), None, 1 << 24, 16, 16, None) == -2  # 2^32 rows
+    assert L.densitykv_cache_read(r(_cache(api, num_seqs=8)), None, 1 << 23, 16, 16, None) == -2   # 2^33 threads
+    assert write(T=1 << 24, most=1 << 23, cache=_cache(api, num_kv_heads=16)) == -2                # likewise
     assert L.densitykv_cache_read(r(c), None, 4, None, 16, None) == -1
     assert L.densitykv_cache_read(r(c), None, 4, 16, 8, None) == -1
     assert L.densitykv_cache_read(r(c), None, 0, None, None, None) == 0
@@ -105,6 +108,7 @@ def test_attention_refusals(L):
     assert attend(window=-1) == -2 and attend(n_sink=-1) == -2 and attend(window=(1 << 30) + 1) == -2
     assert attend(T=1 << 24, num_heads=128) == -2 and attend(num_heads=1 << 20) == -2
     assert attend(T=1 << 20, most=1 << 20, num_heads=1024) == -2   # 2 sequences x 2^20 x 1024 rows
+    assert attend(T=1 << 24, most=1 << 24, num_heads=32, cache=_cache(api, num_kv_heads=32, dtype=1)) == -2  # 2^33 threads
     for scale in (0.0, -1.0, float("nan"), float("inf")):
         assert attend(softmax_scale=scale) == -5
     assert attend(q=None) == -1 and attend(out=None) == -1 and attend(q=24) == -1 and attend(out=24) == -1

@@ -277,6 +277,10 @@ def test_max_new_bounds_the_rows_of_a_sequence():
     out = torch.full_like(q, 3.0)
     api.cache_attention(s.cache, q, start, max_new=12, out=out)
     assert (out[22:] == 3).all() and not (out[:22] == 3).all(-1).any()
+    q, dirty = q[:28], torch.full((28, 1, 64), float("nan"), device="cuda", dtype=torch.bfloat16)
+    del dirty                                           # the allocator gives its memory to the next output
+    got = api.cache_attention(s.cache, q, max_new=12)   # 14 rows each: the last two are left out, and zeros
+    assert (got[12:14] == 0).all() and (got[26:] == 0).all() and not (got[:12] == 0).all(-1).any()
 
 
 # ---- attention ------------------------------------------------------------------------------------------------------
