@@ -3,7 +3,13 @@
 // out = softmax(q K^T * scale) V over the tokens that a query sees (dkv_cache.hpp:
 // seen_by) and the live slots of its bank.  The rows of one (sequence, kv head) are
 // its (token, query head) pairs, tokens first; a row block of them walks key tiles in
-// the order bank, first tokens, window with a streaming softmax in fp32.
+// the order bank, first tokens, window with a streaming softmax in fp32:
+//   m' = max(m, max_j s_j),  w_j = exp(s_j - m'),
+//   l' = l exp(m - m') + sum_j w_j,  o' = o exp(m - m') + sum_j w_j v_j,  out = o / l.
+// Partial results (m, l, o) of disjoint keys join by the same rule, so the keys of a row
+// block may lie over waves (k_cache_attn_few, k_cache_attn_f32) and over workgroups (splits,
+// k_cache_combine).  Many rows are bound by the matrix cores, a single token's rows by the
+// reading of the cache, small calls by the latency of a launch; the figures are at each kernel.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -616,7 +622,16 @@ __device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const
 
 // ---------------------------------------------------------------------------
 // Many rows (bf16): a workgroup of 8 waves owns 256 rows, 32 per wave, and walks tiles of
-// 64 keys that its waves load together.
+// 64 keys that its waves load together.  256 rows read a tile once for 8 waves, so the L2 sees
+// an eighth of what the matrix cores take from LDS; 32 rows a wave are what fits 256 registers
+// (128 columns: 64 of outputs, 32 each of scores and queries, 16 of weights), two waves a SIMD.
+// Measured: bf16, 12 heads x 4,680 tokens over 15,600 keys, d = 128, 228 workgroups: 445 us, 1,008
+// TFLOP/s (a large library product: 1,175; the matrix pipe is busy 47% of the cycles of the 228 CUs,
+// the rest is a tile's softmax and its barrier).  8-bit pages, 12 x 1,560 over 9,360 bank and 9,360
+// cache keys: 214 us with the joining of three splits, 838 TFLOP/s: the conversion of a tile runs
+// between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
+// half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks, 60-65 us, 400 TFLOP/s.
+// Four waves a SIMD at d = 64 (128 registers) would spill 50 to 90 of them.
 // ---------------------------------------------------------------------------
 constexpr int kWWaves = 8, kWRows = 32 * kWWaves, kWK = 64, kWLeast = 4;
 
@@ -1014,8 +1029,12 @@ struct Wave32 {
 };
 
 // ---------------------------------------------------------------------------
-// Few rows, and fp32: a workgroup of 4 waves owns 32 rows; each wave walks tiles of 32 keys of
-// its own (every fourth), and the four results are joined at the end.
+// Few rows, and fp32: a workgroup of 4 waves owns up to 32 rows; each wave walks tiles of 32 keys
+// of its own (every fourth), and the four results are joined at the end.  No wave waits for another
+// before that, so the loads of all are in flight the whole time.  Measured: 64 sequences x 32 heads
+// on 8 over 8,192 tokens of 8 bits: 166 us, 4.98 TB/s of cache (826 MB; a large read reaches 6.0, a copy
+// 4.65); 2 x 32 heads on 8 over 131,071 tokens in bf16, 16 splits: 185 us, 5.34 TB/s; one token of 12
+// heads over 1,028 tokens of 4 bits: 13 us, of which two launches are 8.
 // ---------------------------------------------------------------------------
 constexpr int kFWaves = 4, kFK = 32, kFLeast = 4;
 
@@ -1048,9 +1067,9 @@ struct Block {
   }
 };
 
-// The four waves' results (in LDS, 16 rows of D floats a wave in lo, 16 more in hi; 16-byte chunk j of row r at j ^ (r % 8); wml: maxima and
-// sums) joined under their common maximum, and written out, or as partial results of a split call.  unit: the factor
-// of the maxima's unit to log2.
+// The four waves' results (in LDS, 16 rows of D floats a wave in lo, 16 more in hi; 16-byte chunk j of row r at
+// j ^ (r % 8); wml: maxima and sums) joined under their common maximum, and written out, or as partial results of a
+// split call.  unit: the factor of the maxima's unit to log2.
 template <int DT, int D, int R>
 __device__ __forceinline__ void join_waves(const char *lo, const char *hi, const float2 (*wml)[R], const Block<R> &k, const Pages &c,
                                            const CacheQueries &qs, const Part &part, float unit) {
@@ -1256,7 +1275,9 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
 
 // ---------------------------------------------------------------------------
 // fp32: 32 rows per workgroup, the keys over its four waves, scores and products on
-// v_mfma_f32_32x32x2_f32.  Lane (h, n) holds row n; K step 16 kk + j takes the dims 16 kk + j
+// v_mfma_f32_32x32x2_f32 (all of it in fp32: 4 x 600 causal tokens of d = 128 take 120 us; one
+// wave a SIMD, so its loads, matrix work and softmax partly add up).  32 tokens over 3,000 keys of
+// 8 heads: 172 us, 3.8 TB/s, and as much with 8-bit pages, which are bound by the products.  Lane (h, n) holds row n; K step 16 kk + j takes the dims 16 kk + j
 // (h = 0) and 16 kk + 8 + j of both operands.  Rows of fp32 go to LDS (keys, a tile ahead) or
 // to registers (values, asked for before the scores); quantised rows are exact in bf16 and go
 // through LDS so.
@@ -1563,8 +1584,9 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mas
   join_waves<DKV_F32, D, 32>(lo, hi, wml, k, c, qs, part, 1.0f);  // maxima in log2 units
 }
 
-// Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  D / 4 lanes
-// per row and split; SG splits of a row at a time, joined in LDS.  RB rows per row block, KT keys per tile of the
+// Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  Bound by the
+// launch (4-5 us) up to some megabytes of partial results, then by reading them (18,720 rows x 3 splits x 128 columns,
+// 29 MB: 9.5 us, 3 TB/s).  D / 4 lanes per row and split; SG splits of a row at a time, joined in LDS.  RB rows per row block, KT keys per tile of the
 // kernel that wrote them.
 template <int DT, int D, int RB, int KT, int LEAST, int SG>
 __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit,
