@@ -75,7 +75,7 @@ struct Piece {
 // The piece of this workgroup; false where none is left.  The pieces of all sequences are numbered one after the other
 // (row blocks fastest), without gaps for sequences that have fewer than the longest, and each XCD (workgroup L runs on
 // XCD L % 8) takes an equal run of them: row blocks that read the same keys share an L2, and no XCD has more work than
-// the others.  (5 sequences of 388 to 777 tokens, 16 heads on 4: 107 us with a gap for every missing row block, which
+// the others.  (5 sequences of up to 777 tokens, 16 heads on 4: 107 us with a gap for every missing row block, which
 // gives some XCDs 33 pieces and others 22.)  Every wave takes part.
 template <int R>
 __device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs, int nsplit, Piece &w) {
@@ -133,13 +133,15 @@ __device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs,
 }
 
 // The host sizes the splits by the largest sequence; of them a row block takes as many as
-// leave each at least LEAST tiles (one at least), in equal runs.
+// are full with LEAST tiles each (one at least), in equal runs of whole rounds of ROUND tiles (one
+// for each wave that has tiles of its own).
 template <int LEAST>
 __device__ __forceinline__ int splits_used(int total, int nsplit) {
-  return max(1, min(nsplit, total / LEAST));
+  return max(1, min(nsplit, (total + LEAST - 1) / LEAST));
 }
+template <int ROUND>
 __device__ __forceinline__ void split_range(int total, int used, int split, int &t0, int &t1) {
-  const int per = (total + used - 1) / used;
+  const int per = ((total + used - 1) / used + ROUND - 1) / ROUND * ROUND;
   t0 = min(total, split * per);
   t1 = min(total, t0 + per);
 }
@@ -170,7 +172,7 @@ struct PageWindow {
     tiles = 0;
     gone = 0;
   }
-  // Columns col .. col + 3 may be asked for after seek(col) (col a multiple of 4, or a tile in one page); one call for
+  // Columns col .. col + 7 may be asked for after seek(col) (those of a tile; col a multiple of their number); one call for
   // each tile, followed by its loads, two of them at least.  After eight tiles at least 16 loads are younger than that of
   // `next`: all but the 16 youngest being done, it is there, and the tiles on their way are not waited for.  Earlier (the
   // window may begin soon behind the first tokens) the numbers are loaded again.
@@ -521,12 +523,17 @@ __device__ __forceinline__ void purge(Rows<D> &r, char *vt, const uint32_t *vis,
   if (!has_nonfinite<kBytes>(vt)) return;
   if (work) {
 #pragma unroll 1
-    for (int t2 = 0; t2 < D / 32; ++t2) {
+    for (int e = 0; e < (D / 32) * ((NSUB + 1) / 2); ++e) {  // column tile, 64 keys
+      const int t2 = e % (D / 32), st0 = 4 * (e / (D / 32));
       f32x16 kinds = {};
 #pragma unroll 1
-      for (int st = 0; st < 2 * NSUB; ++st) {
+      for (int st = st0; st < st0 + (NSUB < 2 ? 2 : 4); ++st) {
         u32x4 a = v_operand<D>(vt, st >> 1, st & 1, t2), bv;
-        const uint32_t w = (NSUB > 1 && st >= 2 ? vis[NSUB - 1] : vis[0]) >> (16 * (st & 1));
+        uint32_t w = vis[0];
+#pragma unroll
+        for (int u = 1; u < NSUB; ++u)
+          if (st >> 1 == u) w = vis[u];
+        w >>= 16 * (st & 1);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           a[e] = kind_of(a[e] & 0xffffu) | (kind_of(a[e] >> 16) << 16);
@@ -622,23 +629,28 @@ __device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const
 
 // ---------------------------------------------------------------------------
 // Many rows (bf16): a workgroup of 8 waves owns 256 rows, 32 per wave, and walks tiles of
-// 64 keys that its waves load together.  256 rows read a tile once for 8 waves, so the L2 sees
+// 64 keys (d = 64: 128) that its waves load together.  256 rows read a tile once for 8 waves, so the L2 sees
 // an eighth of what the matrix cores take from LDS; 32 rows a wave are what fits 256 registers
-// (128 columns: 64 of outputs, 32 each of scores and queries, 16 of weights), two waves a SIMD.
+// (128 columns: 64 of outputs, 32 each of scores and queries, 16 of weights), two waves a SIMD;
+// 128 keys fit them at d = 64 and halve the barriers and the softmax's fixed part (12 heads x 4,680
+// tokens over 15,600 keys: 324 -> 287 us, with 8-bit pages 342 -> 312).
 // Measured: bf16, 12 heads x 4,680 tokens over 15,600 keys, d = 128, 228 workgroups: 445 us, 1,008
 // TFLOP/s (a large library product: 1,175; the matrix pipe is busy 47% of the cycles of the 228 CUs,
 // the rest is a tile's softmax and its barrier).  8-bit pages, 12 x 1,560 over 9,360 bank and 9,360
-// cache keys: 214 us with the joining of three splits, 838 TFLOP/s: the conversion of a tile runs
+// cache keys: 212 us with the joining of three splits, 846 TFLOP/s: the conversion of a tile runs
 // between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
-// half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks, 60-65 us, 400 TFLOP/s.
+// half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks of 478 to 777 tokens that see
+// 2,000 tokens each, 62 us, 400 TFLOP/s (13 us before the first product, 200 workgroups of 18 tiles).
 // Four waves a SIMD at d = 64 (128 registers) would spill 50 to 90 of them.
 // ---------------------------------------------------------------------------
-constexpr int kWWaves = 8, kWRows = 32 * kWWaves, kWK = 64, kWLeast = 4;
+constexpr int kWWaves = 8, kWRows = 32 * kWWaves;
+constexpr int wide_keys(int D) { return D == 64 ? 128 : 64; }   // per tile
+constexpr int wide_least(int D) { return 256 / wide_keys(D); }  // tiles of a split
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Mask mask, BankRows bank, CacheQueries qs,
                                                                     int nsplit, Part part) {
-  constexpr int TB = kWK * 2 * D;
+  constexpr int KT = wide_keys(D), NSUB = KT / 32, TB = KT * 2 * D;
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   Piece w;
   if (!my_piece<kWRows>(c, qs, nsplit, w)) return;
@@ -647,11 +659,11 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const int nrows = min(nr.n, c.max_new) * qs.G, r0 = w.rb * kWRows;
   const int len = uni(seq_length(c, s));
   const int r1 = min(r0 + kWRows, nrows) - 1;
-  const Plan pl = uni(plan_of<kWK>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G));
-  const int used = splits_used<kWLeast>(pl.total, nsplit);
+  const Plan pl = uni(plan_of<KT>(mask, bank, b, len, nr.n, r0 / qs.G, r1 / qs.G));
+  const int used = splits_used<wide_least(D)>(pl.total, nsplit);
   if (split >= used) return;
   int tb, nt;
-  split_range(pl.total, used, split, tb, nt);
+  split_range<1>(pl.total, used, split, tb, nt);
   tb = uni(tb), nt = uni(nt);
 
   __shared__ __attribute__((aligned(1024))) char k0[TB], k1[TB], k2[TB];
@@ -680,40 +692,41 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const unsigned char *bk = static_cast<const unsigned char *>(bank.k) + (size_t)b * bank.cap * (2 * D);
   const unsigned char *bv = static_cast<const unsigned char *>(bank.v) + (size_t)b * bank.cap * (2 * D);
 
-  const int kcols = max(1, kWK >> c.lps);  // pages that a tile lies in
+  const int kcols = max(1, KT >> c.lps);  // pages that a tile lies in
   const Seen bfirst = seen_by(mask, len, nr.n, r0 / qs.G), blast = seen_by(mask, len, nr.n, r1 / qs.G);
   auto compute = [&](bool isbank, int t, const char *kt, char *vt, uint32_t absent) __attribute__((always_inline)) {
-    const int pos = tile_pos(pl, kWK, t);
-    const bool act = work && (isbank || !wm.none(pos, kWK));
+    const int pos = tile_pos(pl, KT, t);
+    const bool act = work && (isbank || !wm.none(pos, KT));
     // whether every row of the workgroup sees all of the tile: the same for all its waves
-    const bool whole = isbank || (absent == 0 && pos + kWK <= bfirst.hi && (pos >= blast.lo || pos + kWK <= mask.sink));
-    uint32_t pb[2][8];
-    uint32_t vis[2] = {0, 0};
+    const bool whole = isbank || (absent == 0 && pos + KT <= bfirst.hi && (pos >= blast.lo || pos + KT <= mask.sink));
+    uint32_t pb[NSUB][8];
+    uint32_t vis[NSUB] = {};
     if (act) {
-      f32x16 sc[2];
-      scores<D, 2>(kt, qf, sc);
+      f32x16 sc[NSUB];
+      scores<D, NSUB>(kt, qf, sc);
       if (isbank) {
-        const int nv = pl.m - t * kWK;
-        if (nv < kWK) mask_bank<2>(sc, nv);
+        const int nv = pl.m - t * KT;
+        if (nv < KT) mask_bank<NSUB>(sc, nv);
         rows.any = true;
       } else if (whole) {
         rows.any = true;
       } else {
-        vis[0] = visible_bits(wm, pos, 0, absent, c.lps, lh);
-        vis[1] = visible_bits(wm, pos + 32, 32, absent, c.lps, lh);
-        rows.any |= mask_cache<2>(sc, vis);
+#pragma unroll
+        for (int u = 0; u < NSUB; ++u) vis[u] = visible_bits(wm, pos + 32 * u, 32 * u, absent, c.lps, lh);
+        rows.any |= mask_cache<NSUB>(sc, vis);
       }
-      softmax_update<D, 2>(rows, sc, pb, qs.scale_log2);
+      softmax_update<D, NSUB>(rows, sc, pb, qs.scale_log2);
     }
-    if (!whole) purge<D, 2, 64 * kWWaves>(rows, vt, vis, act);
-    if (act) product<D, 2>(rows, pb, vt);
+    if (!whole) purge<D, NSUB, 64 * kWWaves>(rows, vt, vis, act);
+    if (act) product<D, NSUB>(rows, pb, vt);
   };
 
   // Tiles [t0, t1) of rows held in bf16 go global -> LDS without registers, three stages: two
-  // tiles in flight while one is used.  A wave loads 8 rows of each tile, which lie in one page.
+  // tiles in flight while one is used.  A wave loads KT / 8 (8 or 16) rows of each tile, which lie in one page.
   const Rows8<D> ld = rows8_offsets<D>();
   const PoolAt pool(c, h, FULL ? 2 * D : Quarter<FULL ? DKV_CACHE_FP8 : FMT, D>::kRow);
   auto run_direct = [&](int t0, int t1) __attribute__((always_inline)) {
+    constexpr int kOwn = KT / kWWaves;
     uint32_t pr[3] = {0, 0, 0};
     // Every call has the same number of loads (behind the last tile they read nothing and leave
     // zeros), so that the waits can count them.
@@ -723,25 +736,28 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       uint32_t absent = 0;
       if (t < t1) {
         if (!FULL || t < pl.nb) {
-          const int r8 = t * kWK + 8 * wave;
-          kp = bk + (size_t)r8 * (2 * D), vp = bv + (size_t)r8 * (2 * D);
-          valid = bound(pl.m - r8, 0, 8);
+          const int r = t * KT + kOwn * wave;
+          kp = bk + (size_t)r * (2 * D), vp = bv + (size_t)r * (2 * D);
+          valid = bound(pl.m - r, 0, kOwn);
         } else {
-          const int pos = tile_pos(pl, kWK, t), p8 = pos + 8 * wave;
+          const int pos = tile_pos(pl, KT, t), p = pos + kOwn * wave;
           pw.seek(pos >> c.lps);
-          valid = 8;
-          if (pw.gone != 0 || pos < pl.lo || pos + kWK > pl.hi) {
+          valid = kOwn;
+          if (pw.gone != 0 || pos < pl.lo || pos + KT > pl.hi) {
             absent = pw.absent(pos >> c.lps, kcols);
-            valid = !pw.absent(p8 >> c.lps, 1) && (p8 + 8 > pl.lo || p8 < mask.sink) ? bound(pl.hi - p8, 0, 8) : 0;
+            valid = !pw.absent(p >> c.lps, 1) && (p + kOwn > pl.lo || p < mask.sink) ? bound(pl.hi - p, 0, kOwn) : 0;
           }
-          const size_t off = pool.at(pw.page(p8 >> c.lps), p8);
+          const size_t off = pool.at(pw.page(p >> c.lps), p);
           kp = c.k + off, vp = c.v + off;
         }
       }
-      rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp, vp, valid, 8 * wave, kd, vd);
+#pragma unroll
+      for (int g = 0; g < kOwn / 8; ++g)
+        rows8_issue<D>(ld.rsub, ld.pc, ld.v, kp + g * (16 * D), vp + g * (16 * D), bound(valid - 8 * g, 0, 8),
+                       kOwn * wave + 8 * g, kd, vd);
       return absent;
     };
-    constexpr int kTileLoads = 2 * Rows8<D>::kLoads;
+    constexpr int kTileLoads = kOwn / 8 * 2 * Rows8<D>::kLoads;
     auto step = [&](int t, const char *kt, char *vt, uint32_t absent, char *kn, char *vn) __attribute__((always_inline)) {
       __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0(kTileLoads));  // the next tile may still be on its way
       stage_barrier();
@@ -767,63 +783,72 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
       run_direct(tb, t0);
       stage_barrier();
     }
-    // Quantised rows come through registers, a tile or two ahead, and are stored as bf16: waves 0-3
-    // a quarter row of K per lane, waves 4-7 of V, each wave 16 rows that lie in one page.  Of
-    // the two waves of a SIMD one converts before its matrix work and one after it.
+    // Quantised rows come through registers, a tile ahead (a second one does not fit beside the scores), and
+    // are stored as bf16: waves 0-3 a quarter row of K per lane and 16 rows, waves 4-7 of V; 16 rows lie in one page.
+    // Of the two waves of a SIMD one converts before its matrix work and one after it.
+    constexpr int kQ = KT / 64;
     const bool isv = wave >= 4;
-    const int row16 = 16 * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
-    constexpr int kAhead = D == 64 ? 2 : 1;  // tiles in registers; two of them do not fit beside 128 columns
-    struct {
-      Quarter<FMT, D> x;
-      uint32_t absent;
-    } f[kAhead];
-    auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
-      size_t row = 0;
-      int valid = 0;
-      y.absent = 0;
+    const int row16 = 16 * kQ * (wave & 3), lr = row16 + (l >> 2), qpart = l & 3;
+    Quarter<FMT, D> x[kQ];
+    uint32_t ahead = 0;  // absent pages of the tile in registers
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+      size_t row[kQ] = {};
+      int valid[kQ] = {};
+      ahead = 0;
       if (t < nt) {
-        const int pos = tile_pos(pl, kWK, t), p16 = pos + row16;
+        const int pos = tile_pos(pl, KT, t), p16 = pos + row16;
         pw.seek(pos >> c.lps);
-        valid = 16;
-        if (pw.gone != 0 || pos < pl.lo || pos + kWK > pl.hi) {
-          y.absent = pw.absent(pos >> c.lps, kcols);
-          valid = !pw.absent(p16 >> c.lps, 1) && (p16 + 16 > pl.lo || p16 < mask.sink) ? bound(pl.hi - p16, 0, 16) : 0;
+#pragma unroll
+        for (int g = 0; g < kQ; ++g) valid[g] = 16;
+        if (pw.gone != 0 || pos < pl.lo || pos + KT > pl.hi) {
+          ahead = pw.absent(pos >> c.lps, kcols);
+#pragma unroll
+          for (int g = 0; g < kQ; ++g) {
+            const int p = p16 + 16 * g;
+            valid[g] = !pw.absent(p >> c.lps, 1) && (p + 16 > pl.lo || p < mask.sink) ? bound(pl.hi - p, 0, 16) : 0;
+          }
         }
-        row = pool.at(pw.page(p16 >> c.lps), p16);
+#pragma unroll
+        for (int g = 0; g < kQ; ++g) row[g] = pool.at(pw.page((p16 + 16 * g) >> c.lps), p16 + 16 * g);
       }
-      y.x.load((isv ? c.v : c.k) + row, (isv ? c.vs : c.ks) + row / (Quarter<FMT, D>::kRow / (D / kGroup)), valid, l >> 2, qpart);
+#pragma unroll
+      for (int g = 0; g < kQ; ++g)
+        x[g].load((isv ? c.v : c.k) + row[g], (isv ? c.vs : c.ks) + row[g] / (Quarter<FMT, D>::kRow / (D / kGroup)), valid[g],
+                  l >> 2, qpart);
+    };
+    auto store = [&](auto V, char *tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < kQ; ++g) x[g].template store<decltype(V)::value>(tile, lr + 16 * g, qpart);
     };
     uint32_t absent = 0;
-    auto step = [&](int t, auto &y, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
-      const uint32_t now = absent, next = y.absent;
-      if (!isv) y.x.template store<false>(kn, lr, qpart);
+    auto step = [&](int t, const char *kt, char *vt, char *kn, char *vn) __attribute__((always_inline)) {
+      const uint32_t now = absent, next = ahead;
+      if (!isv) store(std::false_type(), kn);
       asm volatile("" ::: "memory");
-      if (kAhead == 1 && !isv) fetch(y, t + 2);
+      if (!isv) fetch(t + 2);
       if (t < nt) compute(false, t, kt, vt, now);
-      if (isv) y.x.template store<true>(vn, lr, qpart);
+      if (isv) store(std::true_type(), vn);
       asm volatile("" ::: "memory");
-      if (kAhead == 2 || isv) fetch(y, t + 1 + kAhead);
+      if (isv) fetch(t + 2);
       asm volatile("" ::: "memory");
       absent = next;
       __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's stores have landed
       stage_barrier();
     };
     if (t0 < nt) {
-      fetch(f[0], t0);
-      asm volatile("" ::: "memory");  // the loads in this order, which the waits count on
-      if constexpr (kAhead == 2) fetch(f[kAhead - 1], t0 + 1);
+      fetch(t0);
       asm volatile("" ::: "memory");
-      if (isv) f[0].x.template store<true>(v0, lr, qpart);
-      else f[0].x.template store<false>(k0, lr, qpart);
-      absent = f[0].absent;
+      if (isv) store(std::true_type(), v0);
+      else store(std::false_type(), k0);
+      absent = ahead;
       asm volatile("" ::: "memory");
-      fetch(f[0], t0 + kAhead);
+      fetch(t0 + 1);
       __builtin_amdgcn_s_waitcnt(0xc07f);
       stage_barrier();
     }
     for (int t = t0; t < nt; t += 2) {
-      step(t, f[kAhead - 1], k0, v0, k1, v1);
-      step(t + 1, f[0], k1, v1, k0, v0);
+      step(t, k0, v0, k1, v1);
+      step(t + 1, k1, v1, k0, v0);
     }
   }
   if (!work) return;
@@ -1057,7 +1082,7 @@ struct Block {
     pl = uni(plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G));
     const int used = splits_used<kFLeast>(pl.total, nsplit);
     if (split >= used) return false;
-    split_range(pl.total, used, split, tb, nt);
+    split_range<kFWaves>(pl.total, used, split, tb, nt);
     tb = uni(tb), nt = uni(nt);
     return true;
   }
@@ -1213,29 +1238,29 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
     } f[kAhead];
     const int part4 = l & 3, lr = l >> 2;
     auto fetch = [&](auto &y, int t) __attribute__((always_inline)) {
-      const int pos = tile_pos(k.pl, kFK, t);
-      const bool in = t < k.nt;
+      size_t row[2] = {0, 0};
+      int valid[2] = {0, 0};
       y.absent = 0;
-      bool edge = false;
-      if (in) {
+      if (t < k.nt) {
+        const int pos = tile_pos(k.pl, kFK, t);
         pw.seek(pos >> c.lps);
-        edge = pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi;
-        if (edge) y.absent = pw.absent(pos >> c.lps, kcols);
+        valid[0] = valid[1] = 16;
+        if (pw.gone != 0 || pos < k.pl.lo || pos + kFK > k.pl.hi) {
+          y.absent = pw.absent(pos >> c.lps, kcols);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const int p = pos + 16 * g;
+            valid[g] = !pw.absent(p >> c.lps, 1) && (p + 16 > k.pl.lo || p < mask.sink) ? bound(k.pl.hi - p, 0, 16) : 0;
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) row[g] = pool.at(pw.page((pos + 16 * g) >> c.lps), pos + 16 * g);
       }
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        size_t row = 0;
-        int valid = 0;
-        if (in) {
-          const int p16 = pos + 16 * g;
-          valid = 16;
-          if (edge)
-            valid = !pw.absent(p16 >> c.lps, 1) && (p16 + 16 > k.pl.lo || p16 < mask.sink) ? bound(k.pl.hi - p16, 0, 16) : 0;
-          row = pool.at(pw.page(p16 >> c.lps), p16);
-        }
-        const size_t srow = row / (Quarter<FMT, D>::kRow / (D / kGroup));  // scales: one byte per group
-        y.k[g].load(c.k + row, c.ks + srow, valid, lr, part4);
-        y.v[g].load(c.v + row, c.vs + srow, valid, lr, part4);
+        const size_t srow = row[g] / (Quarter<FMT, D>::kRow / (D / kGroup));  // scales: one byte per group
+        y.k[g].load(c.k + row[g], c.ks + srow, valid[g], lr, part4);
+        y.v[g].load(c.v + row[g], c.vs + srow, valid[g], lr, part4);
       }
     };
     auto step = [&](auto &y, int t) __attribute__((always_inline)) {
@@ -1584,10 +1609,13 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mas
   join_waves<DKV_F32, D, 32>(lo, hi, wml, k, c, qs, part, 1.0f);  // maxima in log2 units
 }
 
+constexpr int kMaxSplit = 64;  // a lane of a wave for each
+
 // Rows of a split attention: the partial outputs under their common maximum, divided by the common sum.  Bound by the
 // launch (4-5 us) up to some megabytes of partial results, then by reading them (18,720 rows x 3 splits x 128 columns,
-// 29 MB: 9.5 us, 3 TB/s).  D / 4 lanes per row and split; SG splits of a row at a time, joined in LDS.  RB rows per row block, KT keys per tile of the
-// kernel that wrote them.
+// 29 MB: 9.5 us, 3 TB/s).  D / 4 lanes per row and split; SG splits of a row at a time, joined in LDS, their maxima all
+// read at once (one after the other, 64 of them, cost 8 us).  RB rows per row block, KT keys per tile of the kernel that
+// wrote them.
 template <int DT, int D, int RB, int KT, int LEAST, int SG>
 __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit,
                                                        Part part) {
@@ -1613,32 +1641,49 @@ __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankR
     }
   }
   const float unit = DT == DKV_BF16 ? qs.scale_log2 : 1.0f;  // the bf16 maxima are raw scores
-  float M = -INFINITY;
-  for (int k = 0; k < used; ++k) M = fmaxf(M, part.ml[k * nrow + row].x);
   float l = 0.0f, a[4] = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int k = sub; k < used; k += SG) {
-    const float2 ml = part.ml[k * nrow + row];
+  auto weight = [&](float mx, float M) { return mx == M ? 1.0f : __builtin_amdgcn_exp2f((mx - M) * unit); };
+  auto add = [&](int k, float w) {
     const float4 x = *reinterpret_cast<const float4 *>(part.o + (k * nrow + row) * D + j);
-    const float w = ml.x == M ? 1.0f : __builtin_amdgcn_exp2f((ml.x - M) * unit);
-    l = __builtin_fmaf(ml.y, w, l);
     a[0] = __builtin_fmaf(x.x, w, a[0]);
     a[1] = __builtin_fmaf(x.y, w, a[1]);
     a[2] = __builtin_fmaf(x.z, w, a[2]);
     a[3] = __builtin_fmaf(x.w, w, a[3]);
-  }
-  if constexpr (SG > 1) {
+  };
+  if constexpr (SG > 1) {  // one row: lane k of every wave takes the maximum and sum of split k, in one latency
+    static_assert(NR == 1 && kMaxSplit <= 64, "");
+    const int kk = threadIdx.x & 63;
+    float2 ml{-INFINITY, 0.0f};
+    if (kk < used) ml = part.ml[kk * nrow + row];
+    float M = ml.x;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    const float w = kk < used ? weight(ml.x, M) : 0.0f;
+    l = kk < used ? ml.y * w : 0.0f;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+    for (int k0 = 0; k0 < used; k0 += SG) {
+      const float wk = __shfl(w, min(k0 + sub, 63), 64);
+      if (k0 + sub < used) add(k0 + sub, wk);
+    }
     __shared__ float4 la[256];
-    __shared__ float ll[256];
     la[threadIdx.x] = float4{a[0], a[1], a[2], a[3]};
-    ll[threadIdx.x] = l;
     __syncthreads();
     if (sub != 0) return;
 #pragma unroll
     for (int k = 1; k < SG; ++k) {
       const float4 x = la[threadIdx.x + k * LR];
-      l += ll[threadIdx.x + k * LR];
       a[0] += x.x, a[1] += x.y, a[2] += x.z, a[3] += x.w;
+    }
+  } else {
+    float M = -INFINITY;
+    for (int k = 0; k < used; ++k) M = fmaxf(M, part.ml[k * nrow + row].x);
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) {
+      const float2 ml = part.ml[k * nrow + row];
+      const float w = weight(ml.x, M);
+      l = __builtin_fmaf(ml.y, w, l);
+      add(k, w);
     }
   }
   if (!live) return;
@@ -1652,13 +1697,12 @@ __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankR
 }
 
 constexpr int kCUs = 256;
-constexpr int kMaxSplit = 64;
 constexpr int kManySplits = 5;  // splits from which a row's partial results are read 8 (d = 64: 16) at a time
 
 // Rows of a (sequence, kv head) up to which blocks of 16 or 32 rows are taken: 64, or 32 where the two stages of bf16
 // rows leave a CU one workgroup (us of 32-row and 256-row blocks, 8 kv heads, up to 8,192 tokens).  8-bit pages, d = 128,
 // 32 sequences: 32 rows 93 and 169, 64 rows 125 and 171, 128 rows 214 and 174; 4 sequences: 28 and 35, 33 and 37, 45 and
-// 44; d = 64, 32 sequences: 64 rows 85 and 135, 128 rows 148 and 137.  bf16 pages, d = 128, 32 sequences: 32 rows 159 and
+// 44; d = 64, 32 sequences: 64 rows 81 and 110, 128 rows 141 and 112.  bf16 pages, d = 128, 32 sequences: 32 rows 159 and
 // 171, 64 rows 228 and 170.
 int few_rows(int fmt, int d) { return fmt == DKV_CACHE_FULL && d == 128 ? 32 : 64; }
 
@@ -1699,7 +1743,7 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
   if constexpr (DT == DKV_BF16) {
     if (R == kWRows) {
       k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
-      if (nsplit > 1) combine<DT, D, kWRows, kWK, kWLeast>(c, mask, bank, qs, nsplit, part, s);
+      if (nsplit > 1) combine<DT, D, kWRows, wide_keys(D), wide_least(D)>(c, mask, bank, qs, nsplit, part, s);
     } else if (R == 32) {
       k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
       if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
@@ -1717,7 +1761,9 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
 }  // namespace
 
 // Splits: the time is about rounds of workgroups over the chip times (tiles per split and
-// some tiles' worth of prologue), plus the joining kernel.
+// some tiles' worth of prologue), plus the joining kernel.  Waves with tiles of their own work in
+// rounds of four: one token of 12 heads over 8,001 tokens of 4 bits 22 -> 14 us, in fp32 2 x 64 rows over 400 keys
+// 17 -> 15 us, against runs that end within a round and a joining that reads the maxima in turn.
 int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask &mask, const BankRows &bank, int nh,
                            size_t *bytes) {
   *bytes = 0;
@@ -1726,7 +1772,8 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   if (nrow == 0) return 1;
   const int RB = block_rows(c, dtype, fmt, d, G);
   const bool few = RB != kWRows;
-  const int KT = few ? kFK : kWK, least = few ? kFLeast : kWLeast;
+  const int KT = few ? kFK : wide_keys(d), least = few ? kFLeast : wide_least(d);
+  const int step = few ? kFWaves : 1;
   int64_t keys = (int64_t)c.cols << c.lps;
   if (mask.window > 0) {
     const int64_t seen = (int64_t)mask.window + (mask.causal ? c.max_new : 0) + mask.sink + KT;
@@ -1736,13 +1783,14 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   const int64_t nwg = ((int64_t)c.max_new * G + RB - 1) / RB * c.S * c.H;
   const int64_t slots = few && (d == 64 || fmt != DKV_CACHE_FULL) && dtype == DKV_BF16 ? 2 * kCUs : kCUs;
   // us per tile of a workgroup, and per workgroup
-  const double tile_us = dtype != DKV_BF16 ? (d == 64 ? 0.8 : 1.3) : (few ? (d == 64 ? 0.4 : 0.7) : (d == 64 ? 1.0 : 1.9));
+  const double tile_us = dtype != DKV_BF16 ? (d == 64 ? 0.8 : 1.3) : (few ? (d == 64 ? 0.4 : 0.7) : (d == 64 ? 2.0 : 1.9));
   const double start_us = few ? 5.0 : 8.0;
   int best = 1;
   double best_cost = 0.0;
-  for (int S = 1; S <= kMaxSplit && (S == 1 || tiles / S >= least); ++S) {
+  for (int S = 1; S <= kMaxSplit && (S == 1 || S <= (tiles + least - 1) / least); ++S) {
     const double rounds = (double)((nwg * S + slots - 1) / slots);
-    double cost = rounds * ((double)((tiles + S - 1) / S) * tile_us + start_us);
+    const int64_t per = ((tiles + S - 1) / S + step - 1) / step * step;  // tiles of a workgroup
+    double cost = rounds * ((double)per * tile_us + start_us);
     if (S > 1) cost += 5.0 + (double)nrow * S * (8.0 * d + 16.0) / 4e6;
     if (S == 1 || cost < 0.95 * best_cost) best = S, best_cost = cost;
   }

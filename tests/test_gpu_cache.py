@@ -424,6 +424,24 @@ def test_visible_infinities_propagate_as_in_the_definition():
     assert torch.equal(got[:, other], clean[:, 0][:, other])
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+def test_many_visible_infinities(dtype, d):
+    """Whole tiles of them, in a column each: a sum of one sign is that infinity, of both NaN; other columns are untouched."""
+    s = Setup([400], 1, d, 16, dtype=dtype)
+    q, start = s.queries([400], 1)
+    clean = api.cache_attention(s.cache, q, start)
+    for column, first, last, x in ((2, 100, 231, "inf"), (5, 100, 231, "-inf"), (9, 130, 251, "inf"), (9, 300, 301, "-inf")):
+        for p in range(first, last):
+            s.cache.v[int(s.table[0][p // 16]), 0, p % 16, column] = float(x)
+    got = api.cache_attention(s.cache, q, start)[:, 0]
+    inf = float("inf")
+    assert (got[100:, 2] == inf).all() and (got[100:, 5] == -inf).all()
+    assert (got[130:300, 9] == inf).all() and torch.isnan(got[300:, 9]).all()
+    assert torch.isfinite(got[:100]).all() and torch.isfinite(got[100:130, 9]).all()
+    other = [j for j in range(d) if j not in (2, 5, 9)]
+    assert torch.equal(got[:, other], clean[:, 0][:, other])
+
+
 def test_scores_of_minus_infinity_alone_are_nan():
     for dtype in ("bf16", "f32"):
         s = Setup([5, 70], 1, 64, 16, dtype=dtype)
