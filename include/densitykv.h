@@ -374,9 +374,10 @@ int densitykv_pair_weight_q23(const float *d2, int64_t n, const dkv_params *prm,
  * with max |x| <= F 2^e (so nothing saturates) and stores x 2^-e rounded to
  * nearest, ties to even: an element is off by at most 2^-4 (FP8) or 2^-2 (FP4) of
  * its value, or half the smallest step (2^-10, 2^-2) times 2^e where that is
- * more.  A group that holds a NaN or an infinity gets the scale byte 255 and
- * reads back as NaN throughout.  What a row stands for is exact in bf16, so
- * every reader sees the same values. */
+ * more.  A finite value that would round to 2^128 takes the largest value below it
+ * that its group can hold, within the same bounds.  A group that holds a NaN or
+ * an infinity gets the scale byte 255 and reads back as NaN throughout.  What a
+ * row stands for is exact in bf16, so every reader sees the same values. */
 typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_cache_format;
 
 /*

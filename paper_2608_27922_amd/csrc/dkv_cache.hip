@@ -67,6 +67,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *_
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = 0.0f;
     }
+    below_infinity<FMT>(f, code);
     const float sc = scale_of(code == kScaleNan ? kScaleBias : code);
     if constexpr (FMT == DKV_CACHE_FP8) *reinterpret_cast<uint2 *>(dst + r * D + 8 * ch) = quantise_fp8(f, sc);
     else *reinterpret_cast<uint32_t *>(dst + r * (D / 2) + 4 * ch) = quantise_fp4(f, sc);

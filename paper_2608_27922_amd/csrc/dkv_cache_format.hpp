@@ -31,6 +31,16 @@ __device__ __forceinline__ int scale_code(float amax) {
   const int code = (int)(u >> 23) - emax + ((u & 0x7fffffu) > frac ? 1 : 0);
   return u >= 0x7f800000u ? kScaleNan : max(code, kScaleBias + kScaleFirst);
 }
+// A group of the largest scale code holds values next to 2^128, which would round up to it: they take the largest value
+// below, 1.875 x 2^127 (e4m3: off by at most 2^-4 of the value) or 1.5 x 2^127 (e2m1: 2^-2), and stay finite.
+template <int FMT>
+__device__ __forceinline__ void below_infinity(float *x, int code) {
+  constexpr int top = kScaleBias + (FMT == DKV_CACHE_FP8 ? 120 : 126);
+  constexpr float most = FMT == DKV_CACHE_FP8 ? 0x1.ep127f : 0x1.8p127f;
+  if (code != top) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = fminf(fmaxf(x[j], -most), most);
+}
 __device__ __forceinline__ float scale_of(int code) { return __uint_as_float((uint32_t)code << 23); }
 
 // Eight elements of a group -> 8 bytes (FP8) or 4 bytes (FP4): x / scale rounded to
