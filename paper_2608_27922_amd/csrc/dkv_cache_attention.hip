@@ -30,6 +30,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 constexpr int kBufferRsrcWord3 = 0x00020000;  // raw buffer, 32-bit data, no swizzle
 constexpr float kLazyLimit = 65536.0f;        // weights of a tile's row under the running reference, see exps()
+constexpr float kFarScore = 4096.0f;          // references from which the rounding of their product shows, see is_far()
 
 // Partial results of split keys: for split s and row (s * max_new + i) * nh + head, the
 // running maximum (bf16: raw scores) and weight sum, and the unnormalised output.
@@ -333,12 +334,12 @@ __device__ __forceinline__ float inv_sum(float l) { return l > 0.0f ? 1.0f / l :
 template <int D>
 struct Rows {
   f32x16 o[D / 32];  // O^T: register i of tile t is element 32 t + 8 (i / 4) + 4 h + i % 4
-  float mrun, lrun;
-  bool any;          // this lane saw a key of its row
+  float mrun, off, lrun;  // reference, its offset in the weights' exponents (see is_far), sum of weights
+  bool any;               // this lane saw a key of its row
   __device__ __forceinline__ void init() {
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) o[t] = f32x16{};
-    mrun = -INFINITY, lrun = 0.0f, any = false;
+    mrun = -INFINITY, off = NAN, lrun = 0.0f, any = false;
   }
   // (maximum, sum) of the row, and the outputs: put(chunk of 4 elements, values)
   __device__ __forceinline__ float2 stats() const {
@@ -410,6 +411,13 @@ __device__ __forceinline__ u32x4 v_operand(const char *vt, int sub, int kst, int
   return u32x4{a[0], a[1], b[0], b[1]};
 }
 
+// The exponents (x - ref) c of the weights are taken as fma(x, c, off), off = -(ref c): the rounding of ref c is one factor
+// for all weights of a row under this reference, 2^-13 at most while |ref c| is below 2^12.  From there on (softmax
+// scales of hundreds, or as large queries) it grows to all that a float holds, so that weights vanish or overflow: such a
+// row keeps off as NaN, which sends it through the path of raised references in every tile, where it takes the
+// difference first.  Rows without a reference yet (-inf) go there too.
+__device__ __forceinline__ bool is_far(float off) { return !(fabsf(off) < kFarScore); }
+
 // Softmax update of one tile of one wave from its scores (masked ones are -inf); pb: the
 // weights in bf16, pairs of registers.  The reference maximum is raised only when a lane's
 // sum of weights exceeds 2^16 (or is not finite): weights and sums stay far from overflow,
@@ -418,15 +426,15 @@ template <int D, int NSUB>
 __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t (*pb)[8], float c) {
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
   float psum = 0.0f;
-  auto exps = [&](float moff) {
+  auto exps = [&](auto exponent) __attribute__((always_inline)) {
     psum = 0.0f;
 #pragma unroll
     for (int sub = 0; sub < NSUB; ++sub) {
       float ps = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i], c, moff));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i + 1], c, moff));
+        const float p0 = __builtin_amdgcn_exp2f(exponent(sc[sub][i]));
+        const float p1 = __builtin_amdgcn_exp2f(exponent(sc[sub][i + 1]));
         pb[sub][i >> 1] = pack_bf16x2(p0, p1);
         // row sum of the bf16 weights that are multiplied into O: their rounding (2^-8) enters
         // numerator and denominator alike
@@ -435,7 +443,7 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
       psum += ps;
     }
   };
-  exps(-r.mrun * c);
+  exps([&](float x) { return __builtin_fmaf(x, c, r.off); });
   const bool over = !(psum <= kLazyLimit);
   if (__any(over)) {
     // only the rows concerned, so that a row's result does not depend on the rows beside it
@@ -455,7 +463,10 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
     for (int t2 = 0; t2 < D / 32; ++t2)
 #pragma unroll
       for (int i = 0; i < 16; ++i) r.o[t2][i] *= corr;
-    exps(-mref * c);
+    const float noff = -mref * c;
+    const bool far = is_far(noff);
+    r.off = far ? NAN : noff;
+    exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
   }
   r.lrun += psum;
 }
@@ -881,7 +892,7 @@ struct Wave16 {
   static constexpr int R = 16;
   bf16x8 qf[D / 32];
   f32x4 o[D / 16];
-  float mrun, lrun;
+  float mrun, off, lrun;
   bool any;
   __device__ __forceinline__ void init(const uint16_t *q, bool ok) {
     const int g = (threadIdx.x & 63) >> 4;
@@ -893,7 +904,7 @@ struct Wave16 {
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) o[t] = f32x4{};
-    mrun = -INFINITY, lrun = 0.0f, any = false;
+    mrun = -INFINITY, off = NAN, lrun = 0.0f, any = false;
   }
   static __device__ __forceinline__ u32x4 v_op(const char *vt, int t) {
     const int l = threadIdx.x & 63, g = l >> 4, cq = l & 15;
@@ -943,17 +954,17 @@ struct Wave16 {
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
     uint32_t pb[4];
     float psum = 0.0f;
-    auto exps = [&](float moff) {
+    auto exps = [&](auto exponent) __attribute__((always_inline)) {
       psum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1)], c, moff));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1) + 1], c, moff));
+        const float p0 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1)]));
+        const float p1 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1) + 1]));
         pb[e] = pack_bf16x2(p0, p1);
         psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[e]), ones, psum, false);
       }
     };
-    exps(-mrun * c);
+    exps([&](float x) { return __builtin_fmaf(x, c, off); });
     const bool over = !(psum <= kLazyLimit);
     if (__any(over)) {  // as softmax_update
       int raise = over;
@@ -970,7 +981,10 @@ struct Wave16 {
       lrun *= corr;
 #pragma unroll
       for (int t = 0; t < D / 16; ++t) o[t] *= corr;
-      exps(-mref * c);
+      const float noff = -mref * c;
+      const bool far = is_far(noff);
+      off = far ? NAN : noff;
+      exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
     }
     lrun += psum;
     if (!whole) purge(vt, vis);

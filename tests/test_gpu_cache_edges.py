@@ -56,3 +56,31 @@ def test_finite_rows_read_back_finite(fmt, dtype):
         g = to_np(t)
         assert np.isfinite(g).all()
         assert (np.abs(g - want) <= allowed).all()
+
+
+@pytest.mark.parametrize("scale", (50.0, 1e3, 1e6))
+@pytest.mark.parametrize("new", (1, 20, 200))
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "full"), ("bf16", "fp8"), ("bf16", "fp4"), ("f32", "full"), ("f32", "fp4")])
+def test_scores_far_from_zero(dtype, fmt, new, scale):
+    """Scores are whole numbers (exact in binary32) and at least one apart, so the largest has the weight 1 and the others
+    at most 2^-72 (scale 50 log2 e > 72) each: the output is its value row within 230 x 2^-72 x max |v| < 2^-61 (|v| < 8),
+    whatever the size of the scaled scores (here up to 2^36)."""
+    rng = np.random.default_rng(new)
+    n, d, G = 230, 64, 2
+    k = rng.choice([-6, -4, -3, -2, -1, 0, 1, 2, 3, 4, 6], (n, 1, d))
+    q = rng.integers(-127, 128, (new, G, d))
+    v = torch.from_numpy(rng.standard_normal((n, 1, d))).to(DT[dtype])
+    c = one_sequence(n, d, fmt, dtype)
+    api.cache_write(c, torch.from_numpy(k).to(DT[dtype]).cuda(), v.cuda())
+    rk, rv = (t[0] for t in api.cache_read(c, n))
+    assert np.array_equal(to_np(rk), k[:, 0])
+    got = api.cache_attention(c, torch.from_numpy(q).to(DT[dtype]).cuda(), softmax_scale=scale)
+    sure = 0
+    for i in range(new):
+        for g in range(G):
+            s = np.sort(k[: n - new + i + 1, 0] @ q[i, g])
+            if s[-1] > s[-2]:
+                best = int((k[: n - new + i + 1, 0] @ q[i, g]).argmax())
+                assert (got[i, g].double() - rv[best].double()).abs().max() < 2.0 ** -61, (i, g)
+                sure += 1
+    assert sure > 0.9 * new * G
