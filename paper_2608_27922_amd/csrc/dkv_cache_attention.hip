@@ -465,7 +465,7 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
       for (int i = 0; i < 16; ++i) r.o[t2][i] *= corr;
     const float noff = -mref * c;
     const bool far = is_far(noff);
-    r.off = far ? NAN : noff;
+    r.off = far || mnew == -INFINITY ? NAN : noff;
     exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
   }
   r.lrun += psum;
@@ -983,7 +983,7 @@ struct Wave16 {
       for (int t = 0; t < D / 16; ++t) o[t] *= corr;
       const float noff = -mref * c;
       const bool far = is_far(noff);
-      off = far ? NAN : noff;
+      off = far || mnew == -INFINITY ? NAN : noff;
       exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
     }
     lrun += psum;
