@@ -437,7 +437,10 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
         const float p1 = __builtin_amdgcn_exp2f(exponent(sc[sub][i + 1]));
         pb[sub][i >> 1] = pack_bf16x2(p0, p1);
         // row sum of the bf16 weights that are multiplied into O: their rounding (2^-8) enters
-        // numerator and denominator alike
+        // numerator and denominator alike.  It is a choice for speed: weights in two parts (two_parts) double
+        // the product with V and cost 432 -> 622 us on the large block, 214 -> 279 on the 8-bit one, and with 32 rows a
+        // wave 232 -> 275 (64 sequences x 64 rows a head, 8 bits), for an error of 1.7 in place of 2.4e-3 (2-norm, of
+        // which the rounding of the outputs to bf16 is 1.66)
         ps = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[sub][i >> 1]), ones, ps, false);
       }
       psum += ps;
@@ -887,6 +890,18 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
 // ---------------------------------------------------------------------------
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
+// A pair of weights as two bf16 numbers each, their leading bits and the rest: 15 bits that the product with V keeps.  The
+// rest of a weight that is not zero is not zero either, so that its product with an infinity is that infinity.  With 16
+// rows a wave the matrix pipe has the time (error 2.4 -> 1.7e-3 as at softmax_update; single tokens of 64 sequences over
+// 8 bits 166 -> 168 us, over 4 bits 116 -> 123, over bf16 289 -> 290).
+__device__ __forceinline__ void two_parts(float p0, float p1, uint32_t &lead, uint32_t &rest) {
+  const uint32_t a = __float_as_uint(p0), b = __float_as_uint(p1);
+  lead = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  const float r0 = fmaxf(p0 - __uint_as_float(a & 0xffff0000u), fminf(p0, 0x1p-126f));
+  const float r1 = fmaxf(p1 - __uint_as_float(b & 0xffff0000u), fminf(p1, 0x1p-126f));
+  rest = pack_bf16x2(r0, r1);
+}
+
 template <int D>
 struct Wave16 {
   static constexpr int R = 16;
@@ -951,8 +966,7 @@ struct Wave16 {
             if (16 * st + 4 * g + i >= nvalid) sc[st][i] = -INFINITY;
       }
     }
-    const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-    uint32_t pb[4];
+    uint32_t pb[4], pl[4];
     float psum = 0.0f;
     auto exps = [&](auto exponent) __attribute__((always_inline)) {
       psum = 0.0f;
@@ -960,8 +974,8 @@ struct Wave16 {
       for (int e = 0; e < 4; ++e) {
         const float p0 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1)]));
         const float p1 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1) + 1]));
-        pb[e] = pack_bf16x2(p0, p1);
-        psum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[e]), ones, psum, false);
+        two_parts(p0, p1, pb[e], pl[e]);
+        psum += p0 + p1;
       }
     };
     exps([&](float x) { return __builtin_fmaf(x, c, off); });
@@ -988,11 +1002,13 @@ struct Wave16 {
     }
     lrun += psum;
     if (!whole) purge(vt, vis);
-    const u32x4 bp = {pb[0], pb[1], pb[2], pb[3]};
+    const u32x4 bp = {pb[0], pb[1], pb[2], pb[3]}, bl = {pl[0], pl[1], pl[2], pl[3]};
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t)
-      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v_op(vt, t)), __builtin_bit_cast(bf16x8, bp),
-                                                     o[t], 0, 0, 0);
+    for (int t = 0; t < D / 16; ++t) {
+      const bf16x8 a = __builtin_bit_cast(bf16x8, v_op(vt, t));
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, bp), o[t], 0, 0, 0);
+      o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, bl), o[t], 0, 0, 0);
+    }
   }
   // As the function of that name for 32 rows.
   __device__ __forceinline__ void purge(char *vt, uint32_t vis) {

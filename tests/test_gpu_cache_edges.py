@@ -84,3 +84,58 @@ def test_scores_far_from_zero(dtype, fmt, new, scale):
                 assert (got[i, g].double() - rv[best].double()).abs().max() < 2.0 ** -61, (i, g)
                 sure += 1
     assert sure > 0.9 * new * G
+
+
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("fmt,new,G", [("full", 1, 1), ("full", 3, 5), ("full", 4, 4), ("fp8", 1, 12), ("fp8", 8, 2), ("fp4", 1, 4),
+                                       ("fp4", 16, 1)])
+def test_few_rows_keep_their_weights(fmt, d, new, G):
+    """Up to 16 rows of a head multiply V by weights of 15 bits: of a weight's two bf16 parts the
+    first is cut off, so the rest is at most 2^-7 of it and is rounded to 2^-8 of itself.  The bounds are those of
+    cache_ref.tolerance with 2^-15 in the place of a rounding to bf16 (2^-8)."""
+    n = 700
+    rng = np.random.default_rng(new)
+    c = one_sequence(n, d, fmt, "bf16", heads=2, page=32)
+    rows = [torch.from_numpy(rng.standard_normal((n, 2, d))).bfloat16().cuda() for _ in range(2)]
+    api.cache_write(c, *rows)
+    k, v = (to_np(t) for t in api.cache_read(c, n))
+    q = torch.from_numpy(rng.standard_normal((new, 2 * G, d))).bfloat16().cuda()
+    got = to_np(api.cache_attention(c, q))
+    for head in range(2 * G):
+        mask = np.arange(n) <= np.arange(n - new, n)[:, None]
+        out, av, big = cache_ref.attention(to_np(q)[:, head], k[head // G], v[head // G], mask, d ** -0.5)
+        w = 2 * (d + 4) * 2.0 ** -24 * big[:, None] + 2.0 ** -19 + n * 2.0 ** -24 + 2.0 ** -15
+        tol = w * (av + np.abs(out)) + 2.0 ** -8 * (np.abs(out) + w * av)
+        assert (np.abs(got[:, head] - out) <= tol).all(), head
+
+
+@pytest.mark.parametrize("fmt", ("full", "fp8"))
+@pytest.mark.parametrize("new", (1, 12, 24, 40))
+def test_infinite_values_seen_by_every_row(fmt, new):
+    """Tiles that all rows see whole: an infinity among the values comes out as that infinity, whatever its weight (the
+    weights of the 16 keys before the last tile's are 1 and smaller powers of two)."""
+    n, d = 320, 64
+    c = one_sequence(n, d, "full", "bf16")
+    k = torch.zeros(n, 1, d, dtype=torch.bfloat16)
+    k[:, 0, 0] = -torch.arange(n).float() % 97
+    v = torch.ones(n, 1, d, dtype=torch.bfloat16)
+    q = torch.zeros(new, 1, d, dtype=torch.bfloat16)
+    q[:, 0, 0] = 1.0
+    v[32, 0, 3] = float("inf")
+    v[33, 0, 4] = -float("inf")
+    v[97 + 64, 0, 5] = float("inf")
+    api.cache_write(c, k.cuda(), v.cuda())
+    if fmt != "full":  # the same keys in 8 bits, the infinities in the bank
+        b = api.Bank(1, n, d)
+        b.k.copy_(k.transpose(0, 1))
+        b.v.copy_(v.transpose(0, 1))
+        b.occupancy.fill_(n)
+        c = one_sequence(1, d, fmt, "bf16")
+        api.cache_write(c, k[:1].cuda(), v[:1].cuda())
+        got = api.cache_attention(c, q.cuda(), bank=b, softmax_scale=0.6931471805599453, causal=False)[:, 0]
+    else:
+        got = api.cache_attention(c, q.cuda(), softmax_scale=0.6931471805599453, causal=False)[:, 0]
+    inf = float("inf")
+    assert (got[:, 3] == inf).all() and (got[:, 4] == -inf).all() and (got[:, 5] == inf).all()
+    rest = [j for j in range(d) if j not in (3, 4, 5)]
+    assert (got[:, rest] == 1).all()
