@@ -419,7 +419,8 @@ typedef struct {
  *             [0, T], rows behind the last sequence's are neither read nor written
  *   max_new   an upper bound of every n_s (it sizes the launch): rows of a sequence
  *             beyond its first max_new are neither read nor written
- *   start     [S + 1] int32 ascending, or NULL: T / S tokens each (T divisible by S)
+ *   start     [S + 1] int32 ascending, or NULL: T / S tokens each (T divisible by S;
+ *             max_new is then T / S where it is more)
  */
 typedef struct {
   int32_t n_tokens;

@@ -214,7 +214,8 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   if (!ch->start && ch->n_tokens % c->num_seqs != 0) return DKV_ERR_SHAPE;
   out->start = ch->start;
   out->T = ch->n_tokens;
-  out->max_new = ch->max_new < ch->n_tokens ? ch->max_new : ch->n_tokens;
+  const int32_t most = ch->start ? ch->n_tokens : ch->n_tokens / c->num_seqs;  // of any sequence
+  out->max_new = ch->max_new < most ? ch->max_new : most;
   if ((int64_t)out->max_new * c->num_kv_heads * c->num_seqs >= kMaxRows) return DKV_ERR_SHAPE;
   return DKV_OK;
 }
