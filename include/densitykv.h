@@ -391,9 +391,9 @@ typedef enum { DKV_CACHE_FULL = 0, DKV_CACHE_FP8 = 1, DKV_CACHE_FP4 = 2 } dkv_ca
  * Rows at or behind the length, and pages that no visible token lies in, may hold
  * anything.  A page may be in several entries of the table as long as no call
  * writes to it through more than one of them.
- * The (token, head) rows of a call, S * max_new of them per head, are limited to
- * 2^31 - 1024, and what a call writes or reads back to about 2^35 elements of K and
- * V together (its launch has less than 2^32 threads): DKV_ERR_SHAPE otherwise.
+ * The (token, head) rows of a call are limited to 2^31 - 1024, and what a call
+ * writes or reads back to about 2^35 elements of K and V together (its launch has
+ * less than 2^32 threads): DKV_ERR_SHAPE otherwise.
  */
 typedef struct {
   int32_t num_seqs;     /* S >= 1 */
@@ -417,8 +417,9 @@ typedef struct {
  * is position length[s] - n_s + i, n_s = start[s + 1] - start[s].
  *   n_tokens  T, rows of the arrays (0..2^24); start is clamped on the device to
  *             [0, T], rows behind the last sequence's are neither read nor written
- *   max_new   an upper bound of every n_s (it sizes the launch): rows of a sequence
- *             beyond its first max_new are neither read nor written
+ *   max_new   an upper bound of every n_s, T where none is known: rows of a sequence
+ *             beyond its first max_new are neither read nor written.  Launches are
+ *             sized by S * max_new or by T, whichever is less
  *   start     [S + 1] int32 ascending, or NULL: T / S tokens each (T divisible by S;
  *             max_new is then T / S where it is more)
  */

@@ -207,7 +207,7 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   if (c->format != DKV_CACHE_FULL && ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3))
     return DKV_ERR_INVALID;
   *out = Pages{static_cast<unsigned char *>(c->k), static_cast<unsigned char *>(c->v), c->k_scale, c->v_scale,
-               c->page_table, c->length, nullptr, c->num_seqs, c->num_kv_heads, c->num_pages, c->max_pages, lps, 0, 0};
+               c->page_table, c->length, nullptr, c->num_seqs, c->num_kv_heads, c->num_pages, c->max_pages, lps, 0, 0, true};
   if (!ch) return DKV_OK;
   constexpr int32_t kMax = 1 << 24;
   if (ch->n_tokens < 0 || ch->n_tokens > kMax || ch->max_new < 0) return DKV_ERR_SHAPE;
@@ -216,7 +216,8 @@ int check_cache(const dkv_cache *c, const dkv_chunk *ch, Pages *out) {
   out->T = ch->n_tokens;
   const int32_t most = ch->start ? ch->n_tokens : ch->n_tokens / c->num_seqs;  // of any sequence
   out->max_new = ch->max_new < most ? ch->max_new : most;
-  if ((int64_t)out->max_new * c->num_kv_heads * c->num_seqs >= kMaxRows) return DKV_ERR_SHAPE;
+  out->by_seq = (int64_t)c->num_seqs * out->max_new <= ch->n_tokens;
+  if (places(*out) * c->num_kv_heads >= kMaxRows) return DKV_ERR_SHAPE;
   return DKV_OK;
 }
 

@@ -22,7 +22,11 @@ struct Pages {
   const int32_t *length;  // [S]
   const int32_t *start;   // [S + 1] or null
   int S, H, P, cols, lps, T, max_new;
+  // Places of the chunk's tokens in a launch: max_new for each sequence where those are no more than T (token i of s at
+  // s max_new + i), else the T packed rows, whose sequence is searched for.
+  bool by_seq;
 };
+DKV_HD int64_t places(const Pages &c) { return c.by_seq ? (int64_t)c.S * c.max_new : c.T; }
 
 DKV_HD int bound(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
@@ -37,6 +41,21 @@ DKV_HD NewRows new_rows(const Pages &c, int s) {
   if (!c.start) return NewRows{s * (c.T / c.S), c.T / c.S};
   const int a = bound(c.start[s], 0, c.T);
   return NewRows{a, bound(c.start[s + 1], a, c.T) - a};
+}
+
+// Largest s in [0, S) with at_most(s), -1 if there is none, where at_most holds up to some s and no further.  probe(lo,
+// step, hi) gives the largest k < N with lo + k step < hi and at_most(lo + k step), or -1: N places side by side, the
+// lanes of a group in the kernels.
+template <int N, class F>
+DKV_HD int last_at_most(int S, F probe) {
+  int lo = 0, hi = S;
+  do {
+    const int step = (hi - lo + N - 1) / N, k = probe(lo, step, hi);
+    if (k < 0) return -1;
+    lo += k * step;
+    hi = hi < lo + step ? hi : lo + step;
+  } while (hi - lo > 1);
+  return lo;
 }
 
 // Page that holds position pos (0 <= pos < cols << lps) of sequence s, -1 if absent.

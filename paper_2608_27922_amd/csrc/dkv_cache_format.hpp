@@ -19,6 +19,19 @@ constexpr int kScaleNan = 255;      // group that held a NaN or an infinity
 // A launch has less than 2^32 threads.
 inline bool grid_fits(int64_t workgroups, int threads) { return workgroups <= 0xffffffffLL / threads; }
 
+// Sequence that packed row t belongs to (the last that begins at or before it: -1 if none does), found by groups of N
+// lanes, 64 / N of them a wave.
+template <int N>
+__device__ __forceinline__ int seq_of(const Pages &c, int t) {
+  const int l = threadIdx.x & 63, lane = l % N;
+  return last_at_most<N>(c.S, [&](int lo, int step, int hi) {
+    const int s = lo + lane * step;
+    const bool ok = s < hi && bound(c.start[s], 0, c.T) <= t;
+    const uint64_t bits = (__ballot(ok) >> (l - lane)) & (~0ull >> (64 - N));
+    return 63 - __clzll((long long)bits);
+  });
+}
+
 // Scale code of a group whose largest magnitude is amax: the smallest exponent e with
 // amax <= F 2^e.  F = 1.75 * 2^8 (e4m3) or 1.5 * 2^2 (e2m1), so with amax = 1.f * 2^a
 // e is a - 8 (a - 2), and one more where 1.f exceeds 1.75 (1.5): a comparison of the

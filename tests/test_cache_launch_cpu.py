@@ -3,8 +3,13 @@ whatever bound of a sequence's part the caller gives."""
 
 import ctypes
 import os
+import shutil
+import subprocess
 
+import numpy as np
 import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -40,3 +45,59 @@ def test_uniform_chunks_take_the_workspace_of_their_parts(L, fmt, d, dtype, S, n
 def test_uniform_chunks_pass_the_limits_of_their_tokens(L):
     assert workspace(L, 200, 8, 64, 200 * 1000, 1000, None)[0] == 0
     assert workspace(L, 200, 8, 64, 200 * 1000, 200 * 1000, None)[0] == 0
+
+
+PROGRAM = r"""
+#include <cstdio>
+#include "dkv_cache.hpp"
+using namespace dkv;
+// stdin: n, then S values, then the value to place: for each the last one at or below it, with 8 and with 64 probes
+template <int N> int find(const int *x, int S, int v, int *rounds) {
+  return last_at_most<N>(S, [&](int lo, int step, int hi) {
+    ++*rounds;
+    int best = -1;
+    for (int k = 0; k < N; ++k)
+      if (lo + k * step < hi && x[lo + k * step] <= v) best = k;
+    return best;
+  });
+}
+int main() {
+  static int x[70000];
+  int S, v;
+  while (scanf("%d", &S) == 1) {
+    for (int i = 0; i < S; ++i)
+      if (scanf("%d", x + i) != 1) return 1;
+    if (scanf("%d", &v) != 1) return 1;
+    int a = 0, b = 0;
+    const int p = find<8>(x, S, v, &a), q = find<64>(x, S, v, &b);
+    printf("%d %d %d %d\n", p, q, a, b);
+  }
+}
+"""
+
+
+def test_search_for_a_row_of_packed_sequences(tmp_path):
+    """The last of equal starts (empty sequences come before the one that has the row), a few rounds for any number of
+    sequences, an end within the array for starts that do not ascend."""
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    src, exe = tmp_path / "search.cpp", tmp_path / "search"
+    src.write_text(PROGRAM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", os.path.join(ROOT, "paper_2608_27922_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+    rng = np.random.default_rng(0)
+    cases = []
+    for S in (1, 2, 7, 8, 9, 63, 64, 65, 200, 4096, 4097, 60000):
+        for most in (1, 3, 50):
+            x = np.cumsum(rng.integers(0, most, S))
+            for v in (-1, 0, int(x[S // 2]), int(x[-1]), int(x[-1]) + 5):
+                cases.append((x, v, True))
+        cases.append((rng.integers(0, 100, S), 50, False))
+    text = "\n".join(f"{len(x)} {' '.join(map(str, x))} {v}" for x, v, _ in cases)
+    lines = subprocess.run([str(exe)], input=text, capture_output=True, text=True, check=True).stdout.splitlines()
+    assert len(lines) == len(cases)
+    for (x, v, ascending), line in zip(cases, lines):
+        p, q, a, b = map(int, line.split())
+        if ascending:
+            assert p == q == int(np.searchsorted(x, v, side="right")) - 1
+        assert -1 <= p < len(x) and -1 <= q < len(x) and a <= 7 and b <= 4

@@ -139,3 +139,63 @@ def test_infinite_values_seen_by_every_row(fmt, new):
     assert (got[:, 3] == inf).all() and (got[:, 4] == -inf).all() and (got[:, 5] == inf).all()
     rest = [j for j in range(d) if j not in (3, 4, 5)]
     assert (got[:, rest] == 1).all()
+
+
+def ragged(S, most, seed, pad=3):
+    """(new tokens, start on the GPU, packed tokens with rows behind the last sequence's)."""
+    rng = np.random.default_rng(seed)
+    new = rng.integers(0, most + 1, S)
+    new[rng.random(S) < 0.3] = 0
+    new[int(rng.integers(S))] = most
+    start = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    return new, start, int(new.sum()) + pad
+
+
+@pytest.mark.parametrize("fmt,dtype,d,H", [("full", "bf16", 128, 1), ("fp8", "bf16", 64, 3), ("fp4", "f32", 128, 2), ("full", "f32", 64, 1)])
+@pytest.mark.parametrize("S,most", [(1, 50), (2, 1), (9, 70), (16, 1), (17, 40), (65, 1), (300, 9), (4097, 2)])
+def test_write_without_a_bound(fmt, dtype, d, H, S, most):
+    """Sequences found from the packed rows: the pages are those of the call that knows the longest sequence."""
+    new, start, T = ragged(S, most, S)
+    x = torch.randn(T, H, d, device="cuda").to(DT[dtype])
+    caches = []
+    for bound in (None, most, T):
+        c = api.PagedCache(S, H, d, S * 5, 5, page_size=16, dtype=DT[dtype], format=fmt)
+        c.page_table.copy_(torch.randperm(S * 5, generator=torch.Generator().manual_seed(1)).view(S, 5))
+        c.length.copy_(torch.from_numpy(new).int() + 7)
+        api.cache_write(c, x, x.flip(0), start, max_new=bound)
+        caches.append(c)
+    for c in caches[1:]:
+        for name in ("k", "v", "k_scale", "v_scale"):
+            a, b = getattr(caches[0], name), getattr(c, name)
+            assert a is None or torch.equal(a, b)
+    k, v = api.cache_read(caches[0], most, torch.full((S,), 7, dtype=torch.int32, device="cuda"))
+    i = torch.arange(most, device="cuda")
+    rows = start[:-1, None] + i
+    here = (rows < start[1:, None])[:, :, None, None]
+    for got, src in ((k, x), (v, x.flip(0))):
+        want = torch.where(here, src[rows.clamp(max=T - 1).long()], 0).transpose(1, 2).reshape(S * H, most, d)
+        if fmt == "full":
+            assert torch.equal(got, want)
+        else:  # (rows are checked bit for bit elsewhere) within half a step of the group's largest value
+            top = want.abs().amax(-1, keepdim=True)
+            assert ((got - want).abs() <= top * (2.0 ** -4 if fmt == "fp8" else 2.0 ** -2)).all()
+
+
+def test_write_of_many_sequences_without_a_bound():
+    """2,048 sequences of 32 tokens on average: S x T x H rows are one workgroup over what a launch can have."""
+    S, T, d = 2048, 65536, 128
+    rng = np.random.default_rng(3)
+    cuts = np.sort(rng.integers(0, T + 1, S - 1))
+    start = torch.tensor(np.concatenate([[0], cuts, [T]]), dtype=torch.int32, device="cuda")
+    new = start[1:] - start[:-1]
+    most = int(new.max())
+    cols = (most + 63) // 64
+    c = api.PagedCache(S, 1, d, S * cols, cols, page_size=64)
+    c.page_table.copy_(torch.arange(S * cols, dtype=torch.int32).view(S, cols))
+    c.length.copy_(new)
+    x = torch.randn(T, 1, d, device="cuda", dtype=torch.bfloat16)
+    api.cache_write(c, x, -x, start)
+    k, v = api.cache_read(c, most)
+    seq = torch.repeat_interleave(torch.arange(S, device="cuda"), new.long())
+    pos = torch.arange(T, device="cuda") - start[seq].long()
+    assert torch.equal(k[seq, pos], x[:, 0]) and torch.equal(v[seq, pos], -x[:, 0])
