@@ -126,7 +126,8 @@ hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, 
   constexpr int kRows = kThreads / (D / 8);
   if (c.max_new == 0) return hipSuccess;
   const auto blocks = [&](int tokens) { return ((int64_t)tokens * c.H + kRows - 1) / kRows; };
-  const bool by = (int64_t)c.S * c.max_new <= 2 * (int64_t)c.T && grid_fits(2 * blocks(c.max_new) * c.S, kThreads);
+  const bool by = !c.start || ((int64_t)c.S * c.max_new <= 2 * (int64_t)c.T &&
+                               grid_fits(2 * blocks(c.max_new) * c.S, kThreads));  // only starts can be searched
   const int64_t nb = blocks(by ? c.max_new : c.T), grid = 2 * nb * (by ? c.S : 1);
   if (!grid_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   if (by) k_cache_write<DT, FMT, D, true><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);

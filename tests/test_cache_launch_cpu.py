@@ -47,6 +47,13 @@ def test_uniform_chunks_pass_the_limits_of_their_tokens(L):
     assert workspace(L, 200, 8, 64, 200 * 1000, 200 * 1000, None)[0] == 0
 
 
+def test_uniform_chunks_are_never_searched(L):
+    """There are no starts to search: 2^23 sequences of a token each are one launch too large, and refused."""
+    from paper_2608_27922_amd import api
+    c = api.DkvCache(1 << 23, 1, 128, 16, 10, 1, 0, 1, 16, 16, 16, 16, 4, 4)
+    assert L.densitykv_cache_write(ctypes.byref(c), ctypes.byref(api.DkvChunk(1 << 23, 1, None)), 16, 16, 128, 128, None) == -2
+
+
 PROGRAM = r"""
 #include <cstdio>
 #include "dkv_cache.hpp"
