@@ -448,7 +448,9 @@ int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n
 
 /* The queries of a densitykv_cache_attention call: [T, num_heads, d] in the cache's
  * dtype, row t of head h at element t * q_token_stride + h * q_head_stride; the
- * output likewise (strides multiples of 16 bytes, pointers 16-byte aligned).
+ * output likewise (strides multiples of 16 bytes, pointers 16-byte aligned).  Rows of
+ * the output do not overlap: its larger stride passes over all the rows that the
+ * smaller one places (DKV_ERR_SHAPE otherwise).
  * Query head h reads the rows of head h / (num_heads / H).
  *   causal     nonzero: a query sees the tokens up to its own position; 0: every
  *              query of a chunk stands at the sequence's last position and sees the

@@ -232,6 +232,20 @@ bool strides_ok(int dtype, int64_t token, int64_t head) {
   return token % per == 0 && head % per == 0;
 }
 
+// Whether rows of d elements at i * si + j * sj (i < ni, j < nj) share no element: the larger stride passes over all the
+// rows that the smaller one places.
+bool rows_apart(int64_t ni, int64_t si, int64_t nj, int64_t sj, int d) {
+  const auto size = [](int64_t x) { return x < 0 ? 0 - (uint64_t)x : (uint64_t)x; };
+  uint64_t a = size(si), b = size(sj), n = (uint64_t)ni;
+  if (ni <= 1) return nj <= 1 || b >= (uint64_t)d;
+  if (nj <= 1) return a >= (uint64_t)d;
+  if (a > b) {
+    const uint64_t t = a;
+    a = b, b = t, n = (uint64_t)nj;
+  }
+  return a >= (uint64_t)d && a <= (b - (uint64_t)d) / (n - 1);  // b >= (n - 1) a + d
+}
+
 // Arguments of an attention over the cache, except its pointers.
 int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dkv_bank *bank, const dkv_cache_queries *qs,
                         Pages *c, Mask *mask, BankRows *rows) {
@@ -255,7 +269,8 @@ int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dk
   if (qs->window < 0 || qs->window > kMax || qs->n_sink < 0 || qs->n_sink > kMax) return DKV_ERR_SHAPE;
   if (!(qs->softmax_scale > 0.0f) || qs->softmax_scale > 1e6f) return DKV_ERR_RANGE;
   if (!strides_ok(cache->dtype, qs->q_token_stride, qs->q_head_stride) ||
-      !strides_ok(cache->dtype, qs->out_token_stride, qs->out_head_stride))
+      !strides_ok(cache->dtype, qs->out_token_stride, qs->out_head_stride) ||
+      !rows_apart(c->T, qs->out_token_stride, qs->num_heads, qs->out_head_stride, cache->head_dim))
     return DKV_ERR_SHAPE;
   *mask = Mask{qs->window, qs->window > 0 ? qs->n_sink : 0, qs->causal ? 1 : 0};
   return DKV_OK;

@@ -54,6 +54,17 @@ def test_uniform_chunks_are_never_searched(L):
     assert L.densitykv_cache_write(ctypes.byref(c), ctypes.byref(api.DkvChunk(1 << 23, 1, None)), 16, 16, 128, 128, None) == -2
 
 
+@pytest.mark.parametrize("ot,oh,T,code", [
+    (1024, 128, 6, 0), (2048, 128, 6, 0), (128, 6 * 128, 6, 0), (128, 1 << 40, 6, 0), (-1024, 128, 6, 0), (1024, -128, 6, 0),
+    (136, 2048, 6, 0), (0, 128, 1, 0),                          # one token: its stride is never used
+    (0, 128, 6, -2), (1024, 0, 6, -2), (0, 0, 6, -2), (1024, 64, 6, -2), (896, 128, 6, -2), (128, 128, 6, -2),
+    (128, 5 * 128, 6, -2), (-896, 128, 6, -2), (64, 1024, 6, -2), (128, (1 << 62) + 128, 6, 0),
+    (-(1 << 63), 128, 6, 0), ((1 << 62) // 3 // 128 * 128, -(1 << 62), 6, -2)])
+def test_rows_of_the_output_are_apart(L, ot, oh, T, code):
+    """Outputs of two rows in the same place would depend on which comes last: refused by every call that has them."""
+    assert workspace(L, 1, 4, 8, T, T, None, ot=ot, oh=oh)[0] == code
+
+
 PROGRAM = r"""
 #include <cstdio>
 #include "dkv_cache.hpp"
