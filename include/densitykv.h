@@ -419,7 +419,8 @@ typedef struct {
  *             [0, T], rows behind the last sequence's are neither read nor written
  *   max_new   an upper bound of every n_s, T where none is known: rows of a sequence
  *             beyond its first max_new are neither read nor written.  Launches are
- *             sized by S * max_new or by T, whichever is less
+ *             sized by S * max_new or by T, whichever is less; an attention's kernel
+ *             follows max_new, or where it is T the mean T / S
  *   start     [S + 1] int32 ascending, or NULL: T / S tokens each (T divisible by S;
  *             max_new is then T / S where it is more)
  */
@@ -475,9 +476,9 @@ typedef struct {
  * sequence and, with a bank (NULL: none), all live slots of bank s * H + h (S * H
  * banks of the cache's head_dim and dtype).  fp32 softmax and sums; in bf16 the
  * softmax weights keep 15 bits in the product with V where a chunk has up to 16 rows
- * (tokens x query heads) per kv head, else they are rounded to bf16 and summed as
- * rounded (an error of 2.4e-3 in the 2-norm in place of 1.7e-3, of which the rounding
- * of the output is 1.66e-3).
+ * per kv head (tokens, max_new or where that is T the mean T / S, x query heads), else
+ * they are rounded to bf16 and summed as rounded (an error of 2.4e-3 in the 2-norm in
+ * place of 1.7e-3, of which the rounding of the output is 1.66e-3).
  * A query that sees nothing gives zeros.  Tokens that a query does not see do not
  * change its result, whatever they hold (NaN and infinities included).
  *

@@ -262,9 +262,7 @@ int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dk
     *rows = BankRows{bank->k, bank->v, bank->occupancy, bank->budget, bank->capacity};
   }
   if (qs->num_heads < 1 || qs->num_heads % c->H != 0) return DKV_ERR_SHAPE;
-  if (qs->num_heads >= (1 << 20) || (int64_t)c->T * qs->num_heads >= kMaxRows ||
-      (int64_t)c->S * c->max_new * qs->num_heads >= kMaxRows)
-    return DKV_ERR_SHAPE;
+  if (qs->num_heads >= (1 << 20) || (int64_t)c->T * qs->num_heads >= kMaxRows) return DKV_ERR_SHAPE;
   constexpr int32_t kMax = 1 << 30;
   if (qs->window < 0 || qs->window > kMax || qs->n_sink < 0 || qs->n_sink > kMax) return DKV_ERR_SHAPE;
   if (!(qs->softmax_scale > 0.0f) || qs->softmax_scale > 1e6f) return DKV_ERR_RANGE;

@@ -58,6 +58,14 @@ DKV_HD int last_at_most(int S, F probe) {
   return lo;
 }
 
+// First slot of sequence s where the row blocks (R rows, `rows` for each token) of packed sequences are numbered one after
+// the other: [slot_base(s), slot_base(s + 1)) holds all of those of s, and one slot at most stays empty.  T rows / R + S
+// slots in all.
+DKV_HD int slot_base(const Pages &c, int rows, int R, int s) {
+  return (int)((uint32_t)bound(c.start[s], 0, c.T) * (uint32_t)rows / (uint32_t)R) + s;
+}
+DKV_HD int64_t packed_slots(const Pages &c, int rows, int R) { return (int64_t)c.T * rows / R + c.S; }
+
 // Page that holds position pos (0 <= pos < cols << lps) of sequence s, -1 if absent.
 DKV_HD int page_of(const Pages &c, int s, int pos) {
   const int p = c.table[(size_t)s * c.cols + (pos >> c.lps)];

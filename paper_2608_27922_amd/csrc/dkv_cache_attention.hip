@@ -32,13 +32,12 @@ constexpr int kBufferRsrcWord3 = 0x00020000;  // raw buffer, 32-bit data, no swi
 constexpr float kLazyLimit = 65536.0f;        // weights of a tile's row under the running reference, see exps()
 constexpr float kFarScore = 4096.0f;          // references from which the rounding of their product shows, see is_far()
 
-// Partial results of split keys: for split s and row (s * max_new + i) * nh + head, the
+// Partial results of split keys: for each split, and row (place of the token, see Pages) * nh + head, the
 // running maximum (bf16: raw scores) and weight sum, and the unnormalised output.
 struct Part {
   float *o;    // [nsplit, rows, D]
   float2 *ml;  // [nsplit, rows]; null without splits
 };
-
 // Values from the caller's arrays are the same for all lanes, but loaded like any others: this makes them
 // known as uniform, and the branches and loops on them scalar.
 __device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -68,68 +67,96 @@ __device__ __forceinline__ int tile_pos(const Plan &p, int KT, int t) {
   return KT * (u < p.a1 ? u : u - p.a1 + p.b0);
 }
 
-// One piece of a call: row block rb of R rows of (sequence, kv head), key split `split`.
+// One piece of a call: row block rb of R rows of (sequence, kv head), key split `split`; place: of the sequence's first
+// token among those of all splits.
 struct Piece {
-  int s, h, rb, split;
+  int s, h, rb, split, place;
   NewRows nr;
 };
-// The piece of this workgroup; false where none is left.  The pieces of all sequences are numbered one after the other
-// (row blocks fastest), without gaps for sequences that have fewer than the longest, and each XCD (workgroup L runs on
-// XCD L % 8) takes an equal run of them: row blocks that read the same keys share an L2, and no XCD has more work than
-// the others.  (5 sequences of up to 777 tokens, 16 heads on 4: 107 us with a gap for every missing row block, which
-// gives some XCDs 33 pieces and others 22.)  Every wave takes part.
+// How the row blocks of all sequences are numbered: `slots` > 0, so many of each sequence (uniform chunks, or one row block
+// each at most); kCounted, without gaps, counted by every workgroup from the starts; kSearched, from slot_base on, found by
+// a search, with an empty slot for some sequences.  Up to 256 sequences are counted: 16 single tokens of 32 heads without a
+// bound take 46 us so and 61 searched (45 with it), 250 chunks of up to 30 tokens 172 and 199 (162); counting costs a wave's
+// scan for each 64 of them, so 250 single tokens are 3 us slower than searched, and 2,000, counted in a loop, took 1,138 us
+// where they take 439 (410 with the bound).
+constexpr int kCounted = 0, kSearched = -1, kCountedSeqs = 256;
+
+// The piece of this workgroup; false where it has none.  The pieces are numbered one sequence after the other (row blocks
+// fastest), and each XCD (workgroup L runs on XCD L % 8) takes an equal run of them: row blocks that read the same keys
+// share an L2, and no XCD has more work than the others (5 sequences of up to 777 tokens, 16 heads on 4, with the row
+// blocks of the longest for each: 107 us, some XCDs have 33 pieces and others 22; 62 without gaps).  Empty slots stand
+// together at the end of a sequence's: spread among the pieces they leave the shader engines uneven (64 single tokens, a
+// quarter more slots than pieces: 213 in place of 169 us).
+// Every wave takes part.
 template <int R>
-__device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs, int nsplit, Piece &w) {
-  const int l = threadIdx.x & 63, per = c.H * nsplit;
+__device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs, int nsplit, int slots, Piece &w) {
+  const int l = threadIdx.x & 63;
+  const unsigned per = (unsigned)(c.H * nsplit), L = blockIdx.x, xcd = L % 8;
   auto blocks = [&](int n) { return (min(n, c.max_new) * qs.G + R - 1) / R; };
-  int total = 0;
-  if (c.start && c.S > 1) {
-    for (int s0 = 0; s0 < c.S; s0 += 64) {
-      int n = s0 + l < c.S ? blocks(new_rows(c, s0 + l).n) : 0;
+  // number of this workgroup's piece among N
+  auto piece = [&](unsigned N) { return L < N ? xcd * (N / 8) + min(xcd, N % 8) + L / 8 : N; };
+  unsigned p;
+  int first = 0;  // row blocks before the sequence's
+  if (slots == kCounted) {
+    constexpr int kLoads = kCountedSeqs / 64;
+    NewRows r[kLoads];
+    int upto[kLoads], total = 0;
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o, 64);
-      total += uni(n);
+    for (int j = 0; j < kLoads; ++j) {
+      r[j] = NewRows{0, 0};
+      if (64 * j + l < c.S) r[j] = new_rows(c, 64 * j + l);
     }
-  } else {
-    total = uni(c.S * blocks(new_rows(c, 0).n));
-  }
-  const unsigned N = (unsigned)total * per, L = blockIdx.x, xcd = L % 8;
-  if (L / 8 >= N / 8 + (xcd < N % 8 ? 1 : 0)) return false;
-  const unsigned p = xcd * (N / 8) + min(xcd, N % 8) + L / 8;
-  int u = (int)(p / per), first = 0, cnt;  // u: which row block of all, counted once per sequence
-  if (c.start && c.S > 1) {
-    for (int s0 = 0;; s0 += 64) {
-      const NewRows r = s0 + l < c.S ? new_rows(c, s0 + l) : NewRows{0, 0};
-      const int n = blocks(r.n);
-      int incl = n;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      upto[j] = 0;
+      if (64 * j >= c.S) continue;
+      int n = blocks(r[j].n);
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(incl, o, 64);
-        if (l >= o) incl += y;
+        const int y = __shfl_up(n, o, 64);
+        if (l >= o) n += y;
       }
-      const uint64_t later = __ballot(first + incl > u);
-      if (later == 0) {
-        first += __builtin_amdgcn_readlane(incl, 63);
-        continue;
+      upto[j] = total + n;
+      total = __builtin_amdgcn_readlane(upto[j], 63);
+    }
+    p = piece((unsigned)total * per);
+    if (p >= (unsigned)total * per) return false;
+    const int u = (int)(p / per);
+    w.s = -1;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      const uint64_t later = __ballot(upto[j] > u);
+      if (w.s < 0 && later != 0) {
+        const int i = __ffsll((unsigned long long)later) - 1;
+        w.s = 64 * j + i;
+        w.nr = NewRows{__builtin_amdgcn_readlane(r[j].first, i), __builtin_amdgcn_readlane(r[j].n, i)};
+        first = __builtin_amdgcn_readlane(upto[j], i) - blocks(w.nr.n);
       }
-      const int i = __ffsll((unsigned long long)later) - 1;
-      w.s = s0 + i;
-      cnt = __builtin_amdgcn_readlane(n, i);
-      first += __builtin_amdgcn_readlane(incl, i) - cnt;
-      w.nr = NewRows{__builtin_amdgcn_readlane(r.first, i), __builtin_amdgcn_readlane(r.n, i)};
-      break;
     }
   } else {
-    cnt = total / c.S;
-    w.s = u / cnt;
-    first = w.s * cnt;
+    p = piece(gridDim.x);
+    if (slots != kSearched) {
+      w.s = (int)(p / ((unsigned)slots * per));
+      first = w.s * slots;
+    } else {
+      const int u = (int)(p / per);
+      w.s = uni(last_at_most<64>(c.S, [&](int lo, int step, int hi) {
+        const int at = lo + l * step;
+        return 63 - __clzll((long long)__ballot(at < hi && slot_base(c, qs.G, R, at) <= u));
+      }));
+      if (w.s < 0) return false;
+      first = uni(slot_base(c, qs.G, R, w.s));
+    }
     const NewRows r = new_rows(c, w.s);
     w.nr = NewRows{uni(r.first), uni(r.n)};
   }
-  const int rest = (int)(p - (unsigned)first * per), hs = rest / cnt;
-  w.rb = cnt - 1 - rest % cnt;  // later row blocks see more under a causal mask: first
+  const unsigned cnt = (unsigned)blocks(w.nr.n), at = p - (unsigned)first * per;
+  if (at >= cnt * per) return false;
+  const int hs = (int)(at / cnt);
+  w.rb = (int)(cnt - 1 - at % cnt);  // later row blocks see more under a causal mask: first
   w.h = hs / nsplit;
   w.split = hs % nsplit;
+  w.place = w.split * (int)places(c) + (c.by_seq ? w.s * c.max_new : w.nr.first);
   return true;
 }
 
@@ -663,11 +690,11 @@ constexpr int wide_least(int D) { return 256 / wide_keys(D); }  // tiles of a sp
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Mask mask, BankRows bank, CacheQueries qs,
-                                                                    int nsplit, Part part) {
+                                                                    int nsplit, int slots, Part part) {
   constexpr int KT = wide_keys(D), NSUB = KT / 32, TB = KT * 2 * D;
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   Piece w;
-  if (!my_piece<kWRows>(c, qs, nsplit, w)) return;
+  if (!my_piece<kWRows>(c, qs, nsplit, slots, w)) return;
   const int s = w.s, h = w.h, b = s * c.H + h, split = w.split;
   const NewRows nr = w.nr;
   const int nrows = min(nr.n, c.max_new) * qs.G, r0 = w.rb * kWRows;
@@ -869,8 +896,7 @@ __global__ __launch_bounds__(64 * kWWaves, 1) void k_cache_attn_wide(Pages c, Ma
   const float2 ml = rows.stats();
   if (!rv) return;
   if (part.ml) {
-    const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
-    const size_t row = (size_t)split * nrow + ((size_t)s * c.max_new + at.i) * qs.nh + at.hq;
+    const size_t row = (size_t)(w.place + at.i) * qs.nh + at.hq;
     if (lh == 0) part.ml[row] = ml;
     rows.outputs([&](int chunk, float4 x) { *reinterpret_cast<float4 *>(part.o + row * D + 4 * chunk) = x; });
     return;
@@ -1096,23 +1122,23 @@ constexpr int kFWaves = 4, kFK = 32, kFLeast = 4;
 // What a workgroup of 4 waves knows about its row block of R rows and its run of key tiles.
 template <int R>
 struct Block {
-  int s, h, b, split, len, here, r0, tb, nt;
+  int s, h, b, place, len, here, r0, tb, nt;
   NewRows nr;
   Plan pl;
   // False where it has nothing to do.
   __device__ __forceinline__ bool init(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs,
-                                       int nsplit) {
+                                       int nsplit, int slots) {
     Piece w;
-    if (!my_piece<R>(c, qs, nsplit, w)) return false;
-    s = w.s, h = w.h, split = w.split, nr = w.nr;
+    if (!my_piece<R>(c, qs, nsplit, slots, w)) return false;
+    s = w.s, h = w.h, place = w.place, nr = w.nr;
     b = s * c.H + h;
     r0 = w.rb * R;
     here = min(R, min(nr.n, c.max_new) * qs.G - r0);
     len = uni(seq_length(c, s));
     pl = uni(plan_of<kFK>(mask, bank, b, len, nr.n, r0 / qs.G, (r0 + here - 1) / qs.G));
     const int used = splits_used<kFLeast>(pl.total, nsplit);
-    if (split >= used) return false;
-    split_range<kFWaves>(pl.total, used, split, tb, nt);
+    if (w.split >= used) return false;
+    split_range<kFWaves>(pl.total, used, w.split, tb, nt);
     tb = uni(tb), nt = uni(nt);
     return true;
   }
@@ -1147,8 +1173,7 @@ __device__ __forceinline__ void join_waves(const char *lo, const char *hi, const
     }
     const RowAt ra = row_at(k.nr, qs, k.h, k.r0 + rr);
     if (part.ml) {
-      const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
-      const size_t row = (size_t)k.split * nrow + ((size_t)k.s * c.max_new + ra.i) * qs.nh + ra.hq;
+      const size_t row = (size_t)(k.place + ra.i) * qs.nh + ra.hq;
       if (j == 0) part.ml[row] = float2{M, lt};
       *reinterpret_cast<float4 *>(part.o + row * D + j) = float4{a[0], a[1], a[2], a[3]};
       continue;
@@ -1166,7 +1191,7 @@ __device__ __forceinline__ void join_waves(const char *lo, const char *hi, const
 // R rows per workgroup: 16 or 32.
 template <int FMT, int D, int R>
 __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1 : 2) void k_cache_attn_few(
-    Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit, Part part) {
+    Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit, int slots, Part part) {
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   constexpr int TB = kFK * 2 * D;  // one tile of K or V
   // Stages of a K and a V tile per wave; the first holds the waves' results at the end.  Arrays of their own, so
@@ -1176,7 +1201,7 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
   __shared__ float2 wml[kFWaves][R];
   __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<R> k;
-  if (!k.init(c, mask, bank, qs, nsplit)) return;
+  if (!k.init(c, mask, bank, qs, nsplit, slots)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l % R;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
@@ -1355,14 +1380,14 @@ __device__ __forceinline__ void rows8_issue_f32(const unsigned char *kp, int val
 
 template <int FMT, int D>
 __global__ __launch_bounds__(64 * kFWaves, 1) void k_cache_attn_f32(Pages c, Mask mask, BankRows bank, CacheQueries qs,
-                                                                   int nsplit, Part part) {
+                                                                   int nsplit, int slots, Part part) {
   constexpr bool FULL = FMT == DKV_CACHE_FULL;
   constexpr int TB = kFK * 4 * D;  // a tile of fp32 keys; a K and a V tile of bf16
   __shared__ __attribute__((aligned(1024))) char k0[kFWaves * TB], k1[FULL ? kFWaves * TB : 16];
   __shared__ float2 wml[kFWaves][32];
   __shared__ __attribute__((aligned(256))) int pages_lds[64 * kFWaves];
   Block<32> k;
-  if (!k.init(c, mask, bank, qs, nsplit)) return;
+  if (!k.init(c, mask, bank, qs, nsplit, slots)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lh = l >> 5, n = l & 31;
   const RowAt at = row_at(k.nr, qs, k.h, k.r0 + min(n, k.here - 1));
   const WaveMask wm = k.wave_mask(mask, qs, at.i);
@@ -1650,20 +1675,27 @@ template <int DT, int D, int RB, int KT, int LEAST, int SG>
 __global__ __launch_bounds__(256) void k_cache_combine(Pages c, Mask mask, BankRows bank, CacheQueries qs, int nsplit,
                                                        Part part) {
   constexpr int LR = D / 4, NR = 256 / LR / SG;  // rows per workgroup
-  const size_t nrow = (size_t)c.S * c.max_new * qs.nh;
+  const size_t nrow = (size_t)places(c) * qs.nh;
   const int lane = threadIdx.x % LR, sub = (threadIdx.x / LR) % SG, rr = threadIdx.x / LR / SG, j = 4 * lane;
   const size_t row = (size_t)blockIdx.x * NR + rr;
-  const unsigned per = (unsigned)c.max_new * qs.nh;  // < 2^31
-  bool live = row < nrow;
+  bool live = row < nrow;  // nrow < 2^31
   int s = 0, i = 0, hq = 0, used = 0;
   NewRows nr{0, 0};
   if (live) {
-    s = (int)(row / per);
-    const unsigned rest = (unsigned)(row - (size_t)s * per);
-    i = (int)(rest / (unsigned)qs.nh), hq = (int)(rest % (unsigned)qs.nh);
-    nr = new_rows(c, s);
+    const unsigned place = (unsigned)row / (unsigned)qs.nh;
+    hq = (int)((unsigned)row % (unsigned)qs.nh);
+    if (c.by_seq) {
+      s = (int)(place / (unsigned)c.max_new), i = (int)(place % (unsigned)c.max_new);
+    } else {
+      s = seq_of<LR>(c, (int)place), i = (int)place;
+    }
+    live = s >= 0;
+    if (live) {
+      nr = new_rows(c, s);
+      if (!c.by_seq) i -= nr.first;
+    }
     const int n = min(nr.n, c.max_new), h = hq / qs.G;
-    live = i < n;
+    live = live && i < n;
     if (live) {
       const int r0 = (i * qs.G + hq - h * qs.G) / RB * RB, r1 = min(r0 + RB, n * qs.G) - 1;
       const Plan pl = plan_of<KT>(mask, bank, s * c.H + h, seq_length(c, s), nr.n, r0 / qs.G, r1 / qs.G);
@@ -1736,9 +1768,14 @@ constexpr int kManySplits = 5;  // splits from which a row's partial results are
 // 171, 64 rows 228 and 170.
 int few_rows(int fmt, int d) { return fmt == DKV_CACHE_FULL && d == 128 ? 32 : 64; }
 
+// New tokens that a call's sequences have: the bound of the longest where the caller knows one, else their mean.
+int new_tokens(const Pages &c) { return c.max_new < c.T ? c.max_new : (int)(((int64_t)c.T + c.S - 1) / c.S); }
+// The mean, and what is less than it.
+int mean_tokens(const Pages &c) { return (int)min((int64_t)c.max_new, ((int64_t)c.T + c.S - 1) / c.S); }
+
 // Rows per row block of a call: 16 or 32 with the keys over the waves, or 256.
 int block_rows(const Pages &c, int dtype, int fmt, int d, int G) {
-  const int64_t rows = (int64_t)c.max_new * G;
+  const int64_t rows = (int64_t)new_tokens(c) * G;
   if (dtype != DKV_BF16) return 32;
   return rows <= 16 ? 16 : (rows <= few_rows(fmt, d) ? 32 : kWRows);
 }
@@ -1747,7 +1784,7 @@ template <int DT, int D, int RB, int KT, int LEAST>
 void combine(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, int nsplit, const Part &part,
              hipStream_t s) {
   constexpr int kGroups = 256 / (D / 4);
-  const int64_t nrow = (int64_t)c.S * c.max_new * qs.nh;  // < 2^31 (checked by the caller)
+  const int64_t nrow = places(c) * qs.nh;  // < 2^31 (checked by the caller)
   if (nsplit >= kManySplits)
     k_cache_combine<DT, D, RB, KT, LEAST, kGroups><<<(unsigned)nrow, 256, 0, s>>>(c, mask, bank, qs, nsplit, part);
   else
@@ -1758,8 +1795,8 @@ void combine(const Pages &c, const Mask &mask, const BankRows &bank, const Cache
 template <int DT, int FMT, int D>
 hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, const CacheQueries &qs, void *ws, int nsplit,
                      hipStream_t s) {
-  const int64_t nrow = (int64_t)c.S * c.max_new * qs.nh;
-  if (nrow == 0) return hipSuccess;
+  const int64_t nrow = places(c) * qs.nh;
+  if (c.T == 0 || c.max_new == 0) return hipSuccess;
   Part part{nullptr, nullptr};
   if (nsplit > 1) {  // the outputs first, then the maxima and sums
     part.o = static_cast<float *>(ws);
@@ -1767,22 +1804,24 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
   }
   const int R = block_rows(c, DT, FMT, D, qs.G);
   const int64_t nrb = ((int64_t)c.max_new * qs.G + R - 1) / R;
-  const int64_t grid = nrb * c.S * c.H * nsplit;
+  const int slots = !c.start || c.S == 1 || nrb == 1 ? (int)nrb : (c.S <= kCountedSeqs ? kCounted : kSearched);
+  const int64_t packed = packed_slots(c, qs.G, R);  // no sequence has more than its slots, so counted ones fit both
+  const int64_t grid = (slots > 0 ? nrb * c.S : (slots == kCounted ? min(nrb * c.S, packed) : packed)) * c.H * nsplit;
   if (!grid_fits(grid, 64 * kWWaves) || (nsplit > 1 && !grid_fits(nrow, 256))) return hipErrorInvalidConfiguration;
   const unsigned g = (unsigned)grid;
   if constexpr (DT == DKV_BF16) {
     if (R == kWRows) {
-      k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
+      k_cache_attn_wide<FMT, D><<<g, 64 * kWWaves, 0, s>>>(c, mask, bank, qs, nsplit, slots, part);
       if (nsplit > 1) combine<DT, D, kWRows, wide_keys(D), wide_least(D)>(c, mask, bank, qs, nsplit, part, s);
     } else if (R == 32) {
-      k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
+      k_cache_attn_few<FMT, D, 32><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, slots, part);
       if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
     } else {
-      k_cache_attn_few<FMT, D, 16><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
+      k_cache_attn_few<FMT, D, 16><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, slots, part);
       if (nsplit > 1) combine<DT, D, 16, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
     }
   } else {
-    k_cache_attn_f32<FMT, D><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, part);
+    k_cache_attn_f32<FMT, D><<<g, 64 * kFWaves, 0, s>>>(c, mask, bank, qs, nsplit, slots, part);
     if (nsplit > 1) combine<DT, D, 32, kFK, kFLeast>(c, mask, bank, qs, nsplit, part, s);
   }
   return hipGetLastError();
@@ -1798,19 +1837,20 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
                            size_t *bytes) {
   *bytes = 0;
   const int G = nh / c.H;
-  const int64_t nrow = (int64_t)c.S * c.max_new * nh;
-  if (nrow == 0) return 1;
+  const int64_t nrow = places(c) * nh;
+  if (c.T == 0 || c.max_new == 0) return 1;
+  const int mean = mean_tokens(c);
   const int RB = block_rows(c, dtype, fmt, d, G);
   const bool few = RB != kWRows;
   const int KT = few ? kFK : wide_keys(d), least = few ? kFLeast : wide_least(d);
   const int step = few ? kFWaves : 1;
   int64_t keys = (int64_t)c.cols << c.lps;
   if (mask.window > 0) {
-    const int64_t seen = (int64_t)mask.window + (mask.causal ? c.max_new : 0) + mask.sink + KT;
+    const int64_t seen = (int64_t)mask.window + (mask.causal ? mean : 0) + mask.sink + KT;
     if (seen < keys) keys = seen;
   }
   const int64_t tiles = (keys + KT - 1) / KT + (bank.cap + KT - 1) / KT;
-  const int64_t nwg = ((int64_t)c.max_new * G + RB - 1) / RB * c.S * c.H;
+  const int64_t nwg = ((int64_t)mean * G + RB - 1) / RB * c.S * c.H;
   const int64_t slots = few && (d == 64 || fmt != DKV_CACHE_FULL) && dtype == DKV_BF16 ? 2 * kCUs : kCUs;
   // us per tile of a workgroup, and per workgroup
   const double tile_us = dtype != DKV_BF16 ? (d == 64 ? 0.8 : 1.3) : (few ? (d == 64 ? 0.4 : 0.7) : (d == 64 ? 2.0 : 1.9));
@@ -1821,7 +1861,7 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
     const double rounds = (double)((nwg * S + slots - 1) / slots);
     const int64_t per = ((tiles + S - 1) / S + step - 1) / step * step;  // tiles of a workgroup
     double cost = rounds * ((double)per * tile_us + start_us);
-    if (S > 1) cost += 5.0 + (double)nrow * S * (8.0 * d + 16.0) / 4e6;
+    if (S > 1) cost += 5.0 + (double)mean * c.S * nh * S * (8.0 * d + 16.0) / 4e6;
     if (S == 1 || cost < 0.95 * best_cost) best = S, best_cost = cost;
   }
   if (best > 1) *bytes = (size_t)nrow * best * (d * 4 + 8);

@@ -54,6 +54,24 @@ def test_uniform_chunks_are_never_searched(L):
     assert L.densitykv_cache_write(ctypes.byref(c), ctypes.byref(api.DkvChunk(1 << 23, 1, None)), 16, 16, 128, 128, None) == -2
 
 
+@pytest.mark.parametrize("fmt,d,dtype", [(0, 128, 0), (1, 128, 0), (2, 64, 0), (0, 64, 1)])
+@pytest.mark.parametrize("S,n", [(2, 1), (8, 1), (16, 1), (64, 1), (3, 40), (5, 600)])
+def test_ragged_chunks_take_the_workspace_of_their_tokens(L, fmt, d, dtype, S, n):
+    """The bound of a sequence's part changes nothing where it is the mean, nor does leaving it out (T)."""
+    for window in (0, 700):
+        exact = workspace(L, S, 8, 32, S * n, n, None, fmt, d, dtype=dtype, window=window)
+        for most in (n, S * n, 1 << 24):
+            assert workspace(L, S, 8, 32, S * n, most, 16, fmt, d, dtype=dtype, window=window) == exact
+
+
+def test_ragged_chunks_pass_the_limits_of_their_tokens(L):
+    for most in (1000, 1500, 200 * 1000, 1 << 24):
+        assert workspace(L, 200, 8, 64, 200 * 1000, most, 16)[0] == 0
+    assert workspace(L, 200, 8, 64, (1 << 25) - 16, 1, 16)[0] == -2      # more than 2^24 tokens
+    assert workspace(L, 1 << 12, 8, 64, 1 << 12, 1 << 12, 16, max_pages=4)[0] == 0
+    assert workspace(L, 2, 8, 128, 1 << 24, 1 << 24, 16)[0] == -2        # 2^31 rows
+
+
 @pytest.mark.parametrize("ot,oh,T,code", [
     (1024, 128, 6, 0), (2048, 128, 6, 0), (128, 6 * 128, 6, 0), (128, 1 << 40, 6, 0), (-1024, 128, 6, 0), (1024, -128, 6, 0),
     (136, 2048, 6, 0), (0, 128, 1, 0),                          # one token: its stride is never used
@@ -63,6 +81,65 @@ def test_uniform_chunks_are_never_searched(L):
 def test_rows_of_the_output_are_apart(L, ot, oh, T, code):
     """Outputs of two rows in the same place would depend on which comes last: refused by every call that has them."""
     assert workspace(L, 1, 4, 8, T, T, None, ot=ot, oh=oh)[0] == code
+
+
+SLOTS = r"""
+#include <cstdio>
+#include "dkv_cache.hpp"
+using namespace dkv;
+// stdin: S T max_new rows R, then S + 1 starts -> the row blocks that the slots come out as: sequence, block, for each slot
+int main() {
+  static int start[5001];
+  int S, T, most, rows, R;
+  if (scanf("%d %d %d %d %d", &S, &T, &most, &rows, &R) != 5) return 1;
+  for (int i = 0; i <= S; ++i)
+    if (scanf("%d", start + i) != 1) return 1;
+  Pages c{};
+  c.start = start, c.S = S, c.T = T, c.max_new = most;
+  for (int u = 0; u < packed_slots(c, rows, R); ++u) {
+    const int s = last_at_most<64>(S, [&](int lo, int step, int hi) {
+      int best = -1;
+      for (int k = 0; k < 64; ++k)
+        if (lo + k * step < hi && slot_base(c, rows, R, lo + k * step) <= u) best = k;
+      return best;
+    });
+    if (s < 0) continue;
+    const int first = slot_base(c, rows, R, s), here = slot_base(c, rows, R, s + 1) - first;
+    const NewRows r = new_rows(c, s);
+    const int n = r.n < most ? r.n : most, blocks = (n * rows + R - 1) / R;
+    if (u - first < here && u - first < blocks) printf("%d %d\n", s, u - first);
+  }
+}
+"""
+
+
+@pytest.mark.parametrize("R", (16, 32, 256))
+def test_every_row_block_has_one_slot(tmp_path, R):
+    """Row blocks of packed sequences, empty ones and rows before the first and behind the last among them, are each found
+    once; starts that do not ascend end too."""
+    if shutil.which("g++") is None:
+        pytest.skip("no host compiler")
+    src, exe = tmp_path / "slots.cpp", tmp_path / "slots"
+    src.write_text(SLOTS)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", os.path.join(ROOT, "paper_2608_27922_amd", "csrc"), str(src),
+                    "-o", str(exe)], check=True)
+
+    def run(S, T, most, rows, start):
+        text = f"{S} {T} {most} {rows} {R} " + " ".join(map(str, start))
+        out = subprocess.run([str(exe)], input=text, capture_output=True, text=True, check=True, timeout=60).stdout
+        return [tuple(map(int, line.split())) for line in out.splitlines()]
+
+    rng = np.random.default_rng(R)
+    for S, most, rows in ((1, 500, 3), (2, 1, 4), (64, 40, 5), (65, 700, 1), (300, 3, 8), (5000, 2, 4)):
+        new = rng.integers(0, most + 1, S)
+        new[rng.random(S) < 0.3] = 0
+        start = np.concatenate([[0], np.cumsum(new)]) + 2
+        T = int(start[-1]) + 7
+        for bound in (most, max(1, most // 2), T):
+            want = [(s, b) for s in range(S) for b in range((min(int(new[s]), bound) * rows + R - 1) // R)]
+            assert run(S, T, bound, rows, start) == want
+    wild = rng.choice([-2 ** 31, -1, 0, 5, 39, 40, 41, 2 ** 31 - 1], 51)
+    assert all(0 <= s < 50 for s, _ in run(50, 40, 40, 6, wild))
 
 
 PROGRAM = r"""

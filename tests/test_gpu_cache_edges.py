@@ -10,6 +10,7 @@ pytestmark = pytest.mark.gpu
 
 import cache_ref  # noqa: E402
 from paper_2608_27922_amd import api  # noqa: E402
+from test_gpu_cache import Setup  # noqa: E402
 
 DT = {"bf16": torch.bfloat16, "f32": torch.float32}
 
@@ -199,3 +200,58 @@ def test_write_of_many_sequences_without_a_bound():
     seq = torch.repeat_interleave(torch.arange(S, device="cuda"), new.long())
     pos = torch.arange(T, device="cuda") - start[seq].long()
     assert torch.equal(k[seq, pos], x[:, 0]) and torch.equal(v[seq, pos], -x[:, 0])
+
+
+def against_definition(s, new, start, T, G, bound, **kw):
+    """The call with the given bound of a sequence's part against the 64-bit definition; rows of no sequence stay."""
+    q = torch.from_numpy(s.rng.standard_normal((T, s.H * G, s.d))).to(DT[s.dtype]).cuda()
+    out = torch.full_like(q, 7.0)
+    api.cache_attention(s.cache, q, start, max_new=bound, out=out, **kw)
+    kw = {("sink" if k == "n_sink" else k): v for k, v in kw.items()}
+    ref, tol = s.expected(q, [int(n) for n in new], G, **kw)
+    n, g = int(sum(new)), to_np(out)
+    assert np.isfinite(g).all() and (g[n:] == 7.0).all()
+    assert (np.abs(g - ref)[:n] <= tol[:n]).all()
+
+
+@pytest.mark.parametrize("fmt,dtype,d,H,G", [("full", "bf16", 64, 1, 3), ("fp8", "bf16", 128, 2, 1), ("fp4", "bf16", 64, 1, 8),
+                                             ("full", "f32", 64, 2, 2), ("fp8", "f32", 128, 1, 1)])
+@pytest.mark.parametrize("S,most", [(1, 50), (2, 1), (9, 70), (16, 1), (17, 40), (64, 3), (65, 1), (200, 9)])
+def test_attention_without_a_bound(fmt, dtype, d, H, G, S, most):
+    """Ragged chunks, a third of the sequences without new tokens, whose longest part the host does not know."""
+    new, start, T = ragged(S, most, S)
+    s = Setup([int(n) + 9 * (i % 4) for i, n in enumerate(new)], H, d, 16, fmt, dtype, seed=S)
+    for bound in (None, T - 1, most):
+        against_definition(s, new, start, T, G, bound)
+    against_definition(s, new, start, T, G, None, window=7, n_sink=2, causal=False)
+
+
+@pytest.mark.parametrize("dtype,fmt,d", [("bf16", "full", 128), ("bf16", "fp8", 64), ("f32", "full", 128), ("f32", "fp4", 64)])
+@pytest.mark.parametrize("new", ([1, 1, 0, 1], [3, 0, 1, 2], [0, 40, 5, 0], [90, 1, 0, 30]))
+def test_split_attention_without_a_bound(dtype, fmt, d, new):
+    """Long sequences, whose partial results lie by packed rows: they are joined for the right sequence."""
+    s = Setup([3000, 2500, 9, 700], 1, d, 16, fmt, dtype, seed=7)
+    start = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    for kw in ({}, dict(window=1500, n_sink=30), dict(bank=s.bank(600, [600, 0, 321, 5]))):
+        against_definition(s, new, start, sum(new) + 2, 4, None, **kw)
+
+
+@pytest.mark.parametrize("dtype,fmt", [("bf16", "fp8"), ("bf16", "full"), ("f32", "full")])
+@pytest.mark.parametrize("S,length", [(64, 700), (16, 4000), (3, 6000), (5000, 40)])
+def test_single_tokens_need_no_bound(dtype, fmt, S, length):
+    """One new token of every sequence: the same bits with the bound, without it, and without starts."""
+    H, G, d = 2, 4, 64
+    cols = (length + 15) // 16
+    c = api.PagedCache(S, H, d, S * cols, cols, page_size=16, dtype=DT[dtype], format=fmt)
+    c.page_table.copy_(torch.randperm(S * cols, generator=torch.Generator().manual_seed(0)).view(S, cols))
+    c.length.fill_(length)
+    x = torch.randn(S * length, 2 * H, d, device="cuda").to(DT[dtype])
+    api.cache_write(c, x[:, :H], x[:, H:])
+    q = torch.randn(S, H * G, d, device="cuda").to(DT[dtype])
+    start = torch.arange(S + 1, dtype=torch.int32, device="cuda")
+    want = api.cache_attention(c, q, start, max_new=1)
+    assert torch.equal(api.cache_attention(c, q, start), want)
+    assert torch.equal(api.cache_attention(c, q), want)
+    padded = torch.cat([q, q[:1], q[:1]])  # rows behind the last sequence
+    got = api.cache_attention(c, padded, start, max_new=1)
+    assert torch.equal(got[:S], want) and (got[S:] == 0).all()
