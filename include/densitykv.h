@@ -433,11 +433,15 @@ typedef struct {
 /*
  * Write the chunk's rows into their pages.  k, v: [T, H, d] in the cache's dtype;
  * row t of head h starts at element t * token_stride + h * head_stride (both
- * multiples of 16 bytes, pointers 16-byte aligned).  Rows at positions below 0 or
- * in absent pages are dropped.
+ * multiples of 16 bytes, pointers 16-byte aligned; the stride of a single token or
+ * head is not used).  Rows at positions below 0 or in absent pages are dropped.
+ * densitykv_cache_write_kv is the same with strides of its own for each tensor.
  */
 int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, const void *v,
                           int64_t token_stride, int64_t head_stride, void *stream);
+int densitykv_cache_write_kv(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, int64_t k_token_stride,
+                             int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                             void *stream);
 
 /*
  * Read the rows of the positions first[s] .. first[s] + n of every sequence (first

@@ -57,7 +57,7 @@ SEQ_WEIGHT_BYTES = 32 << 30     # pairwise-weight bytes the sequential workspace
 ENTRY_POINTS = ("densitykv_workspace_size", "densitykv_workspace_size_policy", "densitykv_score",
                 "densitykv_update_bank", "densitykv_update_bank_noalloc",
                 "densitykv_bank_attention", "densitykv_bank_attention_sink", "densitykv_attention_workspace_size",
-                "densitykv_bank_attention_ws", "densitykv_cache_write", "densitykv_cache_read",
+                "densitykv_bank_attention_ws", "densitykv_cache_write", "densitykv_cache_write_kv", "densitykv_cache_read",
                 "densitykv_cache_attention_workspace_size", "densitykv_cache_attention", "densitykv_pair_weight_q23",
                 "densitykv_status_string")
 
@@ -133,6 +133,8 @@ def lib() -> ctypes.CDLL:
         L.densitykv_bank_attention_ws.argtypes = L.densitykv_bank_attention_sink.argtypes[:-1] + [_vp, ctypes.c_size_t,
                                                                                                   _vp]
         L.densitykv_cache_write.argtypes = [P(DkvCache), P(DkvChunk), _vp, _vp, ctypes.c_int64, ctypes.c_int64, _vp]
+        L.densitykv_cache_write_kv.argtypes = [P(DkvCache), P(DkvChunk), _vp, ctypes.c_int64, ctypes.c_int64, _vp,
+                                               ctypes.c_int64, ctypes.c_int64, _vp]
         L.densitykv_cache_read.argtypes = [P(DkvCache), _vp, ctypes.c_int32, _vp, _vp, _vp]
         L.densitykv_cache_attention_workspace_size.argtypes = [P(DkvCache), P(DkvChunk), P(DkvBank), P(DkvCacheQueries),
                                                                P(ctypes.c_size_t)]
@@ -500,6 +502,8 @@ def _check_rows(cache: PagedCache, t: torch.Tensor, what: str):
     if len(s) != 3 or s[2] != cache.d or t.dtype != cache.dtype or t.device != cache.k.device:
         raise ValueError(f"{what} must be [tokens, heads, head_dim] in the cache's dtype, on its device")
     st = t.stride()
+    if s[0] <= 1 or s[1] <= 1:  # the stride of a single token or head is not used, and may be anything
+        st = (st[0] if s[0] > 1 else 0, st[1] if s[1] > 1 else 0, st[2])
     if st[2] != 1 or (st[0] | st[1]) % (16 // t.element_size()) or p % 16:
         raise ValueError(f"the rows of {what} must be contiguous and start at multiples of 16 bytes")
     return s, st, p
@@ -518,16 +522,14 @@ def _enqueue(cache: PagedCache, where: str, fn, *args):
 
 def cache_write(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
                 max_new: Optional[int] = None):
-    """densitykv_cache_write: the new rows k, v [T, num_kv_heads, d] into their pages, on the current stream.
+    """densitykv_cache_write_kv: the new rows k, v [T, num_kv_heads, d] into their pages, on the current stream.
     `start` [S + 1]: first row of each sequence (None: T / S rows each); `max_new`: a bound of the rows of a sequence."""
     shape, st, pk = _check_rows(cache, k, "k")
     vshape, vst, pv = _check_rows(cache, v, "v")
     if shape[1] != cache.H or vshape != shape:
         raise ValueError("k and v must be [tokens, num_kv_heads, head_dim]")
-    if vst != st:
-        raise ValueError("k and v must have the same strides")
-    _enqueue(cache, "cache_write", lib().densitykv_cache_write, ctypes.byref(cache.c()),
-             ctypes.byref(_chunk(cache, shape[0], start, max_new)), pk, pv, st[0], st[1])
+    _enqueue(cache, "cache_write", lib().densitykv_cache_write_kv, ctypes.byref(cache.c()),
+             ctypes.byref(_chunk(cache, shape[0], start, max_new)), pk, st[0], st[1], pv, vst[0], vst[1])
 
 
 def cache_read(cache: PagedCache, n: int, first: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,

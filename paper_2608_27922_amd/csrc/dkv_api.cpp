@@ -226,10 +226,10 @@ int cache_status(hipError_t e) {
   return e == hipSuccess ? DKV_OK : (e == hipErrorInvalidConfiguration ? DKV_ERR_SHAPE : DKV_ERR_HIP);
 }
 
-// Strides of rows that are read 16 bytes at a time.
-bool strides_ok(int dtype, int64_t token, int64_t head) {
+// Strides of rows that are read 16 bytes at a time; that of a single token or head is not used.
+bool strides_ok(int dtype, int tokens, int64_t token, int heads, int64_t head) {
   const int64_t per = dtype == DKV_BF16 ? 8 : 4;
-  return token % per == 0 && head % per == 0;
+  return (tokens <= 1 || token % per == 0) && (heads <= 1 || head % per == 0);
 }
 
 // Whether rows of d elements at i * si + j * sj (i < ni, j < nj) share no element: the larger stride passes over all the
@@ -266,8 +266,8 @@ int check_cache_queries(const dkv_cache *cache, const dkv_chunk *chunk, const dk
   constexpr int32_t kMax = 1 << 30;
   if (qs->window < 0 || qs->window > kMax || qs->n_sink < 0 || qs->n_sink > kMax) return DKV_ERR_SHAPE;
   if (!(qs->softmax_scale > 0.0f) || qs->softmax_scale > 1e6f) return DKV_ERR_RANGE;
-  if (!strides_ok(cache->dtype, qs->q_token_stride, qs->q_head_stride) ||
-      !strides_ok(cache->dtype, qs->out_token_stride, qs->out_head_stride) ||
+  if (!strides_ok(cache->dtype, c->T, qs->q_token_stride, qs->num_heads, qs->q_head_stride) ||
+      !strides_ok(cache->dtype, c->T, qs->out_token_stride, qs->num_heads, qs->out_head_stride) ||
       !rows_apart(c->T, qs->out_token_stride, qs->num_heads, qs->out_head_stride, cache->head_dim))
     return DKV_ERR_SHAPE;
   *mask = Mask{qs->window, qs->window > 0 ? qs->n_sink : 0, qs->causal ? 1 : 0};
@@ -426,17 +426,25 @@ int densitykv_bank_attention(const dkv_bank *bank, const void *q, int32_t n_quer
                                        softmax_scale, stream);
 }
 
-int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, const void *v,
-                          int64_t token_stride, int64_t head_stride, void *stream) {
+int densitykv_cache_write_kv(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, int64_t k_token_stride,
+                             int64_t k_head_stride, const void *v, int64_t v_token_stride, int64_t v_head_stride,
+                             void *stream) {
   Pages c{};
   if (!chunk) return DKV_ERR_INVALID;
   int rc = check_cache(cache, chunk, &c);
   if (rc) return rc;
-  if (!strides_ok(cache->dtype, token_stride, head_stride)) return DKV_ERR_SHAPE;
+  if (!strides_ok(cache->dtype, c.T, k_token_stride, c.H, k_head_stride) ||
+      !strides_ok(cache->dtype, c.T, v_token_stride, c.H, v_head_stride))
+    return DKV_ERR_SHAPE;
   if (c.max_new > 0 && (!k || !v || !aligned16(k) || !aligned16(v))) return DKV_ERR_INVALID;
-  hipError_t e = launch_cache_write(c, cache->dtype, cache->format, cache->head_dim, k, v, token_stride, head_stride,
-                                    static_cast<hipStream_t>(stream));
+  const NewKv x{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride};
+  hipError_t e = launch_cache_write(c, cache->dtype, cache->format, cache->head_dim, x, static_cast<hipStream_t>(stream));
   return cache_status(e);
+}
+
+int densitykv_cache_write(const dkv_cache *cache, const dkv_chunk *chunk, const void *k, const void *v,
+                          int64_t token_stride, int64_t head_stride, void *stream) {
+  return densitykv_cache_write_kv(cache, chunk, k, token_stride, head_stride, v, token_stride, head_stride, stream);
 }
 
 int densitykv_cache_read(const dkv_cache *cache, const int32_t *first, int32_t n, void *k, void *v, void *stream) {

@@ -21,8 +21,7 @@ constexpr int kThreads = 256;
 // Thread = 8 elements of one row (token, head) of K (z = 0) or V (z = 1).  nb workgroups for each z, and for each sequence
 // where the places are by sequences (BY; the choice at run time cost 10.2 -> 11.0 us on a block of 4,680 tokens).
 template <int DT, int FMT, int D, bool BY>
-__global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *__restrict__ k, const void *__restrict__ v,
-                                                          int64_t ts, int64_t hs, int nb) {
+__global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, NewKv in, int nb) {
   constexpr int CH = D / 8;
   const int part = (int)(blockIdx.x / (unsigned)nb), z = part & 1;
   const int ch = (int)threadIdx.x % CH;
@@ -41,7 +40,8 @@ __global__ __launch_bounds__(kThreads) void k_cache_write(Pages c, const void *_
   if (pos < 0) return;
   // the row is on its way while the page number is
   constexpr int W = DT == DKV_BF16 ? 1 : 2;  // 16-byte words of 8 elements
-  const char *src = static_cast<const char *>(z ? v : k) + ((int64_t)(nr.first + i) * ts + h * hs + 8 * ch) * (2 * W);
+  const char *src = static_cast<const char *>(z ? in.v : in.k) +
+                    ((int64_t)(nr.first + i) * (z ? in.vt : in.kt) + h * (z ? in.vh : in.kh) + 8 * ch) * (2 * W);
   uint4 x[W];
 #pragma unroll
   for (int j = 0; j < W; ++j) x[j] = reinterpret_cast<const uint4 *>(src)[j];
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void k_cache_read(Pages c, const int32_t 
 // empty: searching for the sequence of a row takes a latency more (16 sequences of 150 to 300 tokens, 12 heads, 8 bits:
 // 9.0 us by sequences, 10.5 by packed rows, 28 by sequences with a bound of all the tokens).
 template <int DT, int FMT, int D>
-hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, int64_t hs, hipStream_t s) {
+hipError_t write_impl(const Pages &c, const NewKv &x, hipStream_t s) {
   constexpr int kRows = kThreads / (D / 8);
   if (c.max_new == 0) return hipSuccess;
   const auto blocks = [&](int tokens) { return ((int64_t)tokens * c.H + kRows - 1) / kRows; };
@@ -130,8 +130,8 @@ hipError_t write_impl(const Pages &c, const void *k, const void *v, int64_t ts, 
                                grid_fits(2 * blocks(c.max_new) * c.S, kThreads));  // only starts can be searched
   const int64_t nb = blocks(by ? c.max_new : c.T), grid = 2 * nb * (by ? c.S : 1);
   if (!grid_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
-  if (by) k_cache_write<DT, FMT, D, true><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);
-  else k_cache_write<DT, FMT, D, false><<<(unsigned)grid, kThreads, 0, s>>>(c, k, v, ts, hs, (int)nb);
+  if (by) k_cache_write<DT, FMT, D, true><<<(unsigned)grid, kThreads, 0, s>>>(c, x, (int)nb);
+  else k_cache_write<DT, FMT, D, false><<<(unsigned)grid, kThreads, 0, s>>>(c, x, (int)nb);
   return hipGetLastError();
 }
 template <int DT, int FMT, int D>
@@ -161,10 +161,9 @@ hipError_t by_format(int dtype, int fmt, int d, F f) {
 
 }  // namespace
 
-hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const void *k, const void *v, int64_t ts,
-                              int64_t hs, hipStream_t s) {
+hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const NewKv &x, hipStream_t s) {
   return by_format(dtype, fmt, d, [&](auto dt, auto f, auto dd) {
-    return write_impl<decltype(dt)::value, decltype(f)::value, decltype(dd)::value>(c, k, v, ts, hs, s);
+    return write_impl<decltype(dt)::value, decltype(f)::value, decltype(dd)::value>(c, x, s);
   });
 }
 

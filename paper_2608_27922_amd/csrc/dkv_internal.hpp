@@ -116,8 +116,11 @@ hipError_t launch_attention(const dkv_bank &bank, const void *q, int nq, KvSeg w
                             void *out, float scale, const Geom &g, void *ws, int nsplit, hipStream_t s);
 int attention_splits(const dkv_bank &bank, int nq, int nw, int ns, size_t *bytes);
 // The paged window cache (dkv_cache.hip, dkv_cache_attention.hip).
-hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const void *k, const void *v, int64_t token_stride,
-                              int64_t head_stride, hipStream_t s);
+struct NewKv {  // strides in elements
+  const void *k, *v;
+  int64_t kt, kh, vt, vh;
+};
+hipError_t launch_cache_write(const Pages &c, int dtype, int fmt, int d, const NewKv &x, hipStream_t s);
 hipError_t launch_cache_read(const Pages &c, int dtype, int fmt, int d, const int32_t *first, int n, void *k, void *v,
                              hipStream_t s);
 // Queries and outputs of an attention call; bank: the live slots that every query sees as well (capacity 0: none).

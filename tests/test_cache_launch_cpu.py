@@ -83,6 +83,28 @@ def test_rows_of_the_output_are_apart(L, ot, oh, T, code):
     assert workspace(L, 1, 4, 8, T, T, None, ot=ot, oh=oh)[0] == code
 
 
+def test_strides_of_writes_and_of_single_rows(L):
+    """Each tensor's strides are checked for itself; that of a single token or head is not used and may be anything."""
+    from paper_2608_27922_amd import api
+
+    def write(kt=512, kh=128, vt=512, vh=128, T=6, most=None, H=4, k=16, v=16):
+        c = api.DkvCache(2, H, 128, 64, 10, 5, 0, 1, 16, 32, 4, 8, 4, 4)
+        ch = api.DkvChunk(T, T if most is None else most, 16)
+        return L.densitykv_cache_write_kv(ctypes.byref(c), ctypes.byref(ch), k, kt, kh, v, vt, vh, None)
+
+    assert L.densitykv_cache_write_kv(None, None, 16, 0, 0, 16, 0, 0, None) == -1
+    for name in ("kt", "kh", "vt", "vh"):
+        assert write(**{name: 516}) == -2
+    assert write(k=None) == -1 and write(v=8) == -1
+    # nothing to write: the checks pass and nothing is enqueued
+    assert write(vt=4096, vh=256, most=0) == 0
+    assert write(vt=516, T=1, most=0) == 0 and write(kt=3, vt=516, T=1, most=0) == 0
+    assert write(kh=3, H=1, most=0) == 0 and write(kh=3, H=4, most=0) == -2
+    assert workspace(L, 1, 1, 1, 1, 1, None, qt=3, qh=5, ot=7, oh=9)[0] == 0
+    assert workspace(L, 1, 1, 2, 1, 1, None, qt=3, ot=7)[0] == 0
+    assert workspace(L, 1, 1, 2, 1, 1, None, qh=132)[0] == -2 and workspace(L, 1, 1, 1, 2, 2, None, qt=132)[0] == -2
+
+
 SLOTS = r"""
 #include <cstdio>
 #include "dkv_cache.hpp"

@@ -255,3 +255,29 @@ def test_single_tokens_need_no_bound(dtype, fmt, S, length):
     padded = torch.cat([q, q[:1], q[:1]])  # rows behind the last sequence
     got = api.cache_attention(c, padded, start, max_new=1)
     assert torch.equal(got[:S], want) and (got[S:] == 0).all()
+
+
+@pytest.mark.parametrize("fmt,dtype", [("full", "bf16"), ("fp8", "bf16"), ("fp4", "f32"), ("full", "f32")])
+def test_keys_and_values_of_different_strides(fmt, dtype):
+    """A contiguous k beside a v that is still a view of a projection, and tensors of one token or one head whose unused
+    strides are odd, are written as their contiguous copies are."""
+    H, d = 3, 64
+    x = torch.randn(40, 3 * H + 1, d, device="cuda").to(DT[dtype])
+    long = torch.randn(3 * d + 5, device="cuda").to(DT[dtype])
+    odd = torch.randn(1, 2 * d + 8, device="cuda").to(DT[dtype])
+    pairs = [(x[:, :H].contiguous(), x[:, H:2 * H]), (x[:, 2 * H:3 * H].transpose(0, 1).contiguous().transpose(0, 1), x[:, :H]),
+             (long.as_strided((1, 2, d), (5, d, 1)), long.as_strided((1, 2, d), (3 * d + 1, d, 1), d)),
+             (odd.as_strided((2, 1, d), (d + 8, 3, 1)), odd.as_strided((2, 1, d), (d, 7, 1)))]
+    for k, v in pairs:
+        n, heads = k.shape[:2]
+        a, b = (one_sequence(n, d, fmt, dtype, heads=heads) for _ in range(2))
+        api.cache_write(a, k, v)
+        api.cache_write(b, k.contiguous().clone(), v.contiguous().clone())
+        for p, q in zip(api.cache_read(a, n), api.cache_read(b, n)):
+            assert torch.equal(p, q)
+    q = long.as_strided((1, 2, d), (7, d, 1))
+    out = torch.empty(3 * d, device="cuda", dtype=DT[dtype]).as_strided((1, 2, d), (3, d, 1))
+    c = one_sequence(9, d, fmt, dtype)
+    api.cache_write(c, x[:9, :1], x[:9, 1:2])
+    want = api.cache_attention(c, q.contiguous().clone())
+    assert api.cache_attention(c, q, out=out) is out and torch.equal(out, want)
