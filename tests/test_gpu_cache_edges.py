@@ -281,3 +281,55 @@ def test_keys_and_values_of_different_strides(fmt, dtype):
     api.cache_write(c, x[:9, :1], x[:9, 1:2])
     want = api.cache_attention(c, q.contiguous().clone())
     assert api.cache_attention(c, q, out=out) is out and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("fmt", ("full", "fp8", "fp4"))
+def test_generation_loop_against_the_definition(fmt):
+    """Blocks are written, attended with the bank, read back as they leave the window and enter the bank: every output
+    against the 64-bit definition on the rows as they are held.  The bounds are tight enough to see one key too many or
+    too few: without the first tokens, or with the window a token off, the definition itself lies outside them."""
+    H, d, n, page, blocks = 2, 128, 96, 32, 5
+    window, sink = 2 * n, 20
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    c = api.PagedCache(1, H, d, blocks * n // page, blocks * n // page, page_size=page, format=fmt)
+    bank = api.Bank(H, 150, d, group_size=H)
+    prm = api.Params(sigma2_log2=6)
+    held = [[], []]
+    for t in range(blocks):
+        x = torch.randn(n, 3 * H, d, device="cuda", generator=gen)
+        k = (torch.round(40 * x[:, :H]).clamp(-127, 127) / 64).bfloat16()  # keys on the bank's grid
+        v, q = x[:, H:2 * H].bfloat16(), x[:, 2 * H:].bfloat16()
+        c.page_table[0, t * n // page:(t + 1) * n // page] = torch.randperm(n // page).int() + t * n // page
+        c.length += n
+        api.cache_write(c, k, v)
+        for rows, x in zip(held, (k, v)):
+            x = to_np(x).transpose(1, 0, 2)
+            rows.append(x if fmt == "full" else cache_ref.values(*cache_ref.quantise(x, fmt), fmt))
+        got = to_np(api.cache_attention(c, q, bank=bank, window=window, n_sink=sink, causal=False))
+        live = bank.occupancy.tolist()
+        K, V = (np.concatenate(rows, 1) for rows in held)
+        total = (t + 1) * n
+
+        def definition(h, window, sink):
+            seen = cache_ref.visible(total, n, 0, window, sink, False)
+            k = np.concatenate([to_np(bank.k[h, :live[h]]), K[h, seen]])
+            v = np.concatenate([to_np(bank.v[h, :live[h]]), V[h, seen]])
+            return cache_ref.attention(to_np(q)[:, h], k, v, np.ones((n, len(k)), bool), d ** -0.5), len(k)
+
+        for h in range(H):
+            (out, av, big), m = definition(h, window, sink)
+            tol = cache_ref.tolerance(out, av, big, d, m, "bf16")
+            assert (np.abs(got[:, h] - out) <= tol).all(), (t, h)
+            if total > window + sink:
+                for w, s in ((window, 0), (window, sink - 1), (window - 1, sink), (window + 1, sink)):
+                    other = definition(h, w, s)[0][0]
+                    assert (np.abs(other - out) > tol).any(), (t, h, w, s)
+        if t >= 1:
+            first = torch.tensor([(t - 1) * n], dtype=torch.int32, device="cuda")
+            seg = api.cache_read(c, n, first)
+            for rows, x in zip(held, seg):
+                assert np.array_equal(to_np(x), rows[t - 1])
+            if fmt == "full":  # keys off the grid are accepted too, with rounded decisions
+                assert (seg[0] * 64 == torch.round(seg[0] * 64)).all()
+            api.update_bank(bank, *seg, t - 1, prm)
+    assert int(bank.occupancy.min()) > 0
