@@ -133,6 +133,7 @@ __device__ __forceinline__ bool my_piece(const Pages &c, const CacheQueries &qs,
         first = __builtin_amdgcn_readlane(upto[j], i) - blocks(w.nr.n);
       }
     }
+    if (w.s < 0) return false;  // starts that do not ascend, whose sum overflows
   } else {
     p = piece(gridDim.x);
     if (slots != kSearched) {
