@@ -333,3 +333,56 @@ def test_generation_loop_against_the_definition(fmt):
                 assert (seg[0] * 64 == torch.round(seg[0] * 64)).all()
             api.update_bank(bank, *seg, t - 1, prm)
     assert int(bank.occupancy.min()) > 0
+
+
+@pytest.mark.parametrize("fmt,dtype,S,most,G", [("fp8", "bf16", 300, 60, 4), ("full", "bf16", 257, 20, 1), ("full", "f32", 300, 40, 2),
+                                                ("fp4", "bf16", 256, 90, 4)])
+def test_row_blocks_of_hundreds_of_sequences(fmt, dtype, S, most, G):
+    """Several row blocks a sequence, found by counting up to 256 sequences and by a search beyond."""
+    new, start, T = ragged(S, most, S + most)
+    s = Setup([int(n) + 5 * (i % 3) for i, n in enumerate(new)], 1, 64, 16, fmt, dtype, seed=S)
+    for bound in (None, most):
+        against_definition(s, new, start, T, G, bound, window=50, n_sink=3)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("full", "bf16"), ("fp8", "bf16"), ("full", "f32")])
+def test_captured_ragged_steps_without_a_bound(fmt, dtype):
+    """One graph of a write and an attention for any division of its tokens over the sequences, padded rows included: every
+    replay against the eager calls on the same contents."""
+    S, H, G, d, T, cols = 5, 2, 2, 64, 48, 80
+    caches = [api.PagedCache(S, H, d, S * cols, cols, page_size=16, dtype=DT[dtype], format=fmt) for _ in range(2)]
+    for c in caches:
+        c.page_table.copy_(torch.randperm(S * cols, generator=torch.Generator().manual_seed(2)).view(S, cols))
+    x = torch.zeros(T, (2 + G) * H, d, device="cuda", dtype=DT[dtype])
+    start = torch.zeros(S + 1, dtype=torch.int32, device="cuda")
+    out = torch.zeros(T, H * G, d, device="cuda", dtype=DT[dtype])
+
+    def step(c, out, workspace=None):
+        api.cache_write(c, x[:, :H], x[:, H:2 * H], start)
+        api.cache_attention(c, x[:, 2 * H:], start, window=300, n_sink=4, out=out, workspace=workspace)
+
+    ws = torch.empty(32 << 20, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(caches[0], out, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(caches[0], out, ws)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for t, parts in enumerate(([1, 1, 1, 1, 1], [0, 40, 0, 8, 0], [48, 0, 0, 0, 0], [5, 5, 5, 5, 5], [0, 0, 0, 0, 3], [9, 9, 10, 10, 10])):
+        x.normal_(generator=gen)
+        start.copy_(torch.tensor(np.cumsum([0, *parts])))
+        for c in caches:
+            c.length += torch.tensor(parts, dtype=torch.int32, device="cuda")
+        out.fill_(5.0)
+        graph.replay()
+        want = torch.full_like(out, 5.0)
+        step(caches[1], want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), f"replay {t}"
+        assert (out[sum(parts):] == 5).all()
+        for name in ("k", "v", "k_scale", "v_scale"):
+            a, b = (getattr(c, name) for c in caches)
+            assert a is None or torch.equal(a, b)
