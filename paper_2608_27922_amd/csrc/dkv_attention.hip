@@ -322,6 +322,15 @@ __device__ __forceinline__ void ftile_issue(const uint16_t *base, int nvalid, ch
 // removes the common factor exactly.
 constexpr float kLazyLimit = 65536.0f;
 
+// The exponents (x - ref) c of the weights are taken as fma(x, c, off), off = -(ref c): the rounding
+// of ref c is one factor for all weights of a row under this reference, 2^-13 at most while |ref c| is
+// below 2^12.  From there on (softmax scales of hundreds, or as large queries) it grows to all that a
+// float holds, so that weights vanish or overflow: such a row keeps off as NaN, which sends it through
+// the path of raised references in every tile, where it takes the difference first.  Rows without a
+// reference yet (-inf) go there too.
+constexpr float kFarScore = 4096.0f;
+__device__ __forceinline__ bool is_far(float off) { return !(fabsf(off) < kFarScore); }
+
 // s_waitcnt immediate (gfx9 encoding): at most n vector-memory operations
 // outstanding and no LDS operation outstanding (expcnt left alone).
 constexpr int waitcnt_vm_lgkm0(int n) { return (n & 15) | ((n >> 4) << 14) | (7 << 4); }
@@ -383,7 +392,7 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_attn_mfma(dkv_bank bank, co
   f32x16 o[DT];
 #pragma unroll
   for (int t = 0; t < DT; ++t) o[t] = f32x16{};
-  float mrun = -INFINITY, lrun = 0.0f;
+  float mrun = -INFINITY, off = NAN, lrun = 0.0f;
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
 
   // Tiles never straddle the bank/window boundary: ceil(m/64) bank tiles, then
@@ -462,21 +471,21 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_attn_mfma(dkv_bank bank, co
     }
     uint32_t pb[2][8];
     float psum = 0.0f;
-    auto exps = [&](float moff) {
+    auto exps = [&](auto exponent) __attribute__((always_inline)) {
       float ps[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i], c, moff));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i + 1], c, moff));
+          const float p0 = __builtin_amdgcn_exp2f(exponent(sc[sub][i]));
+          const float p1 = __builtin_amdgcn_exp2f(exponent(sc[sub][i + 1]));
           pb[sub][i >> 1] = pack_bf16x2(p0, p1);
           // row sum of the bf16 weights actually multiplied into O
           ps[sub] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[sub][i >> 1]), ones, ps[sub], false);
         }
       psum = ps[0] + ps[1];
     };
-    exps(-mrun * c);
+    exps([&](float x) { return __builtin_fmaf(x, c, off); });
     if (__any(!(psum <= kLazyLimit))) {
       float tmax = sc[0][0];
 #pragma unroll
@@ -493,7 +502,10 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_attn_mfma(dkv_bank bank, co
       for (int t2 = 0; t2 < DT; ++t2)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t2][i] *= corr;
-      exps(-mref * c);
+      const float noff = -mref * c;
+      const bool far = is_far(noff);
+      off = far || mnew == -INFINITY ? NAN : noff;
+      exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
     }
     lrun += psum;
 #pragma unroll
