@@ -1,12 +1,13 @@
 // Rows of the paged window cache: written (quantised on the way) and read back.
 //
-// Both are one pass over the data with 8 elements per thread: 16 bytes of a bf16 row
-// in or out, so a wave reads and writes whole 128-byte lines on both sides.  The
-// largest magnitude of a group of 32 comes from four neighbouring lanes.  Bound by memory:
-// a write of 8 x 4,680 tokens of 12 heads into 8 bits with its reading back takes 120 us
-// (4.6 TB/s), a reading of 30 layers' blocks out of 4 bits 255 us (4.3 TB/s, 3.4 of it
-// written; a large copy reaches 4.7 on this card).  Two and four rows per thread, with their
-// loads side by side, gained nothing (117 and 256 us).
+// Both are one pass over the data with 8 elements per thread: 16 bytes of a bf16 row in or out.  A write takes the heads of a
+// token one after the other, which lie page_size rows apart in a page: rows of 128 bytes and more go out as whole lines,
+// shorter ones (4 bits, 8 bits at d = 64) as 64 or 32 bytes of one, the scales as 2 or 4.  A reading takes the rows of one
+// head, which lie together.  The largest magnitude of a group of 32 comes from four neighbouring lanes.  Bound by memory.
+// Two sets of buffers in turn, d = 128, 12 heads: 8 x 4,680 tokens into 8 bits 87 us (349 MB, 119 of them written, 4.0 TB/s),
+// in bf16 88 us (460 MB, 5.2 TB/s); read back 50 us (7.0 TB/s: the pages come out of caches in part) and 81 us.  30 layers'
+// blocks into 4 bits 301 us (1,092 MB, 229 written, 3.6 TB/s), read out of them 250 (863 MB written, 4.4 TB/s; a large copy
+// reaches 4.65 on this card).  Two and four rows per thread, with their loads side by side, gained nothing.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -676,13 +676,15 @@ __device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const
 // (128 columns: 64 of outputs, 32 each of scores and queries, 16 of weights), two waves a SIMD;
 // 128 keys fit them at d = 64 and halve the barriers and the softmax's fixed part (12 heads x 4,680
 // tokens over 15,600 keys: 324 -> 287 us, with 8-bit pages 342 -> 312).
-// Measured: bf16, 12 heads x 4,680 tokens over 15,600 keys, d = 128, 228 workgroups: 445 us, 1,008
-// TFLOP/s (a large library product: 1,175; the matrix pipe is busy 47% of the cycles of the 228 CUs,
-// the rest is a tile's softmax and its barrier).  8-bit pages, 12 x 1,560 over 9,360 bank and 9,360
-// cache keys: 212 us with the joining of three splits, 846 TFLOP/s: the conversion of a tile runs
-// between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
+// Measured: bf16, 12 heads x 4,680 tokens over 15,600 keys, d = 128, 228 workgroups: 435 to 470 us on different cards, 960
+// to 1,030 TFLOP/s (a large library product: 1,175; the matrix pipe is busy 47% of the cycles of the 228 CUs,
+// the rest is a tile's softmax and its barrier: both waves of a SIMD come to them together).  8-bit pages, 12 x 1,560 over
+// 9,360 bank and 9,360 cache keys: 217 to 222 us with the joining of three splits, 820 TFLOP/s: the conversion of a tile
+// runs between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
 // half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks of 478 to 777 tokens that see
-// 2,000 tokens each, 62 us, 400 TFLOP/s (13 us before the first product, 200 workgroups of 18 tiles).
+// 2,000 tokens each, 63 us, 393 TFLOP/s (13 us before the first product, 200 workgroups of 18 tiles).
+// No vector register is spilled; 27 to 63 scalar ones are, into lanes of vector registers (kernel arguments, the plan of the
+// tiles and buffer descriptors that stay live over the loops).
 // Four waves a SIMD at d = 64 (128 registers) would spill 50 to 90 of them.
 // ---------------------------------------------------------------------------
 constexpr int kWWaves = 8, kWRows = 32 * kWWaves;
@@ -1114,8 +1116,9 @@ struct Wave32 {
 // Few rows, and fp32: a workgroup of 4 waves owns up to 32 rows; each wave walks tiles of 32 keys
 // of its own (every fourth), and the four results are joined at the end.  No wave waits for another
 // before that, so the loads of all are in flight the whole time.  Measured: 64 sequences x 32 heads
-// on 8 over 8,192 tokens of 8 bits: 166 us, 4.98 TB/s of cache (826 MB; a large read reaches 6.0, a copy
-// 4.65); 2 x 32 heads on 8 over 131,071 tokens in bf16, 16 splits: 185 us, 5.34 TB/s; one token of 12
+// on 8 over 4,096 to 8,192 tokens of 8 bits: 168 us, 4.9 TB/s of cache (826 MB; a large read reaches 6.0, a copy
+// 4.65), of 4 bits 123 us (426 MB: the conversion and the softmax); with a bank of 4,680 in bf16 beside 8 bits 376 us,
+// 5.5 TB/s; 2 x 32 heads on 8 over 131,071 tokens in bf16, 16 splits: 180 us, 5.5 TB/s; one token of 12
 // heads over 1,028 tokens of 4 bits: 13 us, of which two launches are 8.
 // ---------------------------------------------------------------------------
 constexpr int kFWaves = 4, kFK = 32, kFLeast = 4;
@@ -1356,9 +1359,11 @@ __global__ __launch_bounds__(64 * kFWaves, FMT == DKV_CACHE_FULL && D == 128 ? 1
 
 // ---------------------------------------------------------------------------
 // fp32: 32 rows per workgroup, the keys over its four waves, scores and products on
-// v_mfma_f32_32x32x2_f32 (all of it in fp32: 4 x 600 causal tokens of d = 128 take 120 us; one
-// wave a SIMD, so its loads, matrix work and softmax partly add up).  32 tokens over 3,000 keys of
-// 8 heads: 172 us, 3.8 TB/s, and as much with 8-bit pages, which are bound by the products.  Lane (h, n) holds row n; K step 16 kk + j takes the dims 16 kk + j
+// v_mfma_f32_32x32x2_f32 (all of it in fp32; one wave a SIMD, so its loads, matrix work and softmax partly add up).  d = 128:
+// 2,000 causal tokens of 12 heads over 4,000: 527 us, 70 TFLOP/s (a large product: 153).  Single tokens of 64 sequences, 32
+// heads on 8, over 1,500 to 3,000 tokens: 299 us, 4.1 TB/s (a reading: 204); over 8 bits 292 and over 4 bits 287 us, where
+// a reading of the pages takes 53 and 27: 4 rows are padded to 32 in the products, and the values are read from LDS two bytes
+// at a time.  Lane (h, n) holds row n; K step 16 kk + j takes the dims 16 kk + j
 // (h = 0) and 16 kk + 8 + j of both operands.  Rows of fp32 go to LDS (keys, a tile ahead) or
 // to registers (values, asked for before the scores); quantised rows are exact in bf16 and go
 // through LDS so.
