@@ -73,8 +73,8 @@ struct Piece {
   int s, h, rb, split, place;
   NewRows nr;
 };
-// How the row blocks of all sequences are numbered: `slots` > 0, so many of each sequence (uniform chunks, or one row block
-// each at most); kCounted, without gaps, counted by every workgroup from the starts; kSearched, from slot_base on, found by
+// How the row blocks of all sequences are numbered: `slots` > 0, so many of each sequence (uniform chunks, one row block each
+// at most, or where T has many rows of no sequence); kCounted, without gaps, counted by every workgroup from the starts; kSearched, from slot_base on, found by
 // a search, with an empty slot for some sequences.  Up to 256 sequences are counted: 16 single tokens of 32 heads without a
 // bound take 46 us so and 61 searched (45 with it), 250 chunks of up to 30 tokens 172 and 199 (162); counting costs a wave's
 // scan for each 64 of them, so 250 single tokens are 3 us slower than searched, and 2,000, counted in a loop, took 1,138 us
@@ -1810,9 +1810,10 @@ hipError_t attn_impl(const Pages &c, const Mask &mask, const BankRows &bank, con
   }
   const int R = block_rows(c, DT, FMT, D, qs.G);
   const int64_t nrb = ((int64_t)c.max_new * qs.G + R - 1) / R;
-  const int slots = !c.start || c.S == 1 || nrb == 1 ? (int)nrb : (c.S <= kCountedSeqs ? kCounted : kSearched);
-  const int64_t packed = packed_slots(c, qs.G, R);  // no sequence has more than its slots, so counted ones fit both
-  const int64_t grid = (slots > 0 ? nrb * c.S : (slots == kCounted ? min(nrb * c.S, packed) : packed)) * c.H * nsplit;
+  const int64_t even = nrb * c.S, packed = packed_slots(c, qs.G, R);  // slots if all are the longest, or of T rows
+  const bool counted = c.start && c.S > 1 && c.S <= kCountedSeqs && nrb > 1;
+  const int slots = counted ? kCounted : (!c.start || even <= packed ? (int)nrb : kSearched);
+  const int64_t grid = (slots == kSearched || (counted && packed < even) ? packed : even) * c.H * nsplit;
   if (!grid_fits(grid, 64 * kWWaves) || (nsplit > 1 && !grid_fits(nrow, 256))) return hipErrorInvalidConfiguration;
   const unsigned g = (unsigned)grid;
   if constexpr (DT == DKV_BF16) {

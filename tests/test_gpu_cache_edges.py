@@ -386,3 +386,11 @@ def test_captured_ragged_steps_without_a_bound(fmt, dtype):
         for name in ("k", "v", "k_scale", "v_scale"):
             a, b = (getattr(c, name) for c in caches)
             assert a is None or torch.equal(a, b)
+
+
+def test_padded_chunk_of_hundreds_of_sequences():
+    """A buffer of many more rows than tokens: with the bound, the row blocks are numbered by sequences."""
+    new, start, T = ragged(300, 90, 1, pad=20000)
+    s = Setup([int(n) + 5 * (i % 3) for i, n in enumerate(new)], 1, 64, 16, "fp8", "bf16", seed=4)
+    for bound in (90, None):
+        against_definition(s, new, start, T, 4, bound, window=50, n_sink=3)
