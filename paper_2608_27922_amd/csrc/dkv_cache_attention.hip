@@ -1776,8 +1776,6 @@ int few_rows(int fmt, int d) { return fmt == DKV_CACHE_FULL && d == 128 ? 32 : 6
 
 // New tokens that a call's sequences have: the bound of the longest where the caller knows one, else their mean.
 int new_tokens(const Pages &c) { return c.max_new < c.T ? c.max_new : (int)(((int64_t)c.T + c.S - 1) / c.S); }
-// The mean, and what is less than it.
-int mean_tokens(const Pages &c) { return (int)min((int64_t)c.max_new, ((int64_t)c.T + c.S - 1) / c.S); }
 
 // Rows per row block of a call: 16 or 32 with the keys over the waves, or 256.
 int block_rows(const Pages &c, int dtype, int fmt, int d, int G) {
@@ -1846,18 +1844,18 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
   const int G = nh / c.H;
   const int64_t nrow = places(c) * nh;
   if (c.T == 0 || c.max_new == 0) return 1;
-  const int mean = mean_tokens(c);
+  const int news = new_tokens(c);
   const int RB = block_rows(c, dtype, fmt, d, G);
   const bool few = RB != kWRows;
   const int KT = few ? kFK : wide_keys(d), least = few ? kFLeast : wide_least(d);
   const int step = few ? kFWaves : 1;
   int64_t keys = (int64_t)c.cols << c.lps;
   if (mask.window > 0) {
-    const int64_t seen = (int64_t)mask.window + (mask.causal ? mean : 0) + mask.sink + KT;
+    const int64_t seen = (int64_t)mask.window + (mask.causal ? news : 0) + mask.sink + KT;
     if (seen < keys) keys = seen;
   }
   const int64_t tiles = (keys + KT - 1) / KT + (bank.cap + KT - 1) / KT;
-  const int64_t nwg = ((int64_t)mean * G + RB - 1) / RB * c.S * c.H;
+  const int64_t nwg = min(((int64_t)news * G + RB - 1) / RB * c.S, packed_slots(c, G, RB)) * c.H;
   const int64_t slots = few && (d == 64 || fmt != DKV_CACHE_FULL) && dtype == DKV_BF16 ? 2 * kCUs : kCUs;
   // us per tile of a workgroup, and per workgroup
   const double tile_us = dtype != DKV_BF16 ? (d == 64 ? 0.8 : 1.3) : (few ? (d == 64 ? 0.4 : 0.7) : (d == 64 ? 2.0 : 1.9));
@@ -1868,7 +1866,7 @@ int cache_attention_splits(const Pages &c, int dtype, int fmt, int d, const Mask
     const double rounds = (double)((nwg * S + slots - 1) / slots);
     const int64_t per = ((tiles + S - 1) / S + step - 1) / step * step;  // tiles of a workgroup
     double cost = rounds * ((double)per * tile_us + start_us);
-    if (S > 1) cost += 5.0 + (double)mean * c.S * nh * S * (8.0 * d + 16.0) / 4e6;
+    if (S > 1) cost += 5.0 + (double)nrow * S * (8.0 * d + 16.0) / 4e6;
     if (S == 1 || cost < 0.95 * best_cost) best = S, best_cost = cost;
   }
   if (best > 1) *bytes = (size_t)nrow * best * (d * 4 + 8);
