@@ -471,21 +471,21 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_attn_mfma(dkv_bank bank, co
     }
     uint32_t pb[2][8];
     float psum = 0.0f;
-    auto exps = [&](auto exponent) __attribute__((always_inline)) {
+    auto exps = [&](float moff) __attribute__((always_inline)) {
       float ps[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
-          const float p0 = __builtin_amdgcn_exp2f(exponent(sc[sub][i]));
-          const float p1 = __builtin_amdgcn_exp2f(exponent(sc[sub][i + 1]));
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i], c, moff));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i + 1], c, moff));
           pb[sub][i >> 1] = pack_bf16x2(p0, p1);
           // row sum of the bf16 weights actually multiplied into O
           ps[sub] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pb[sub][i >> 1]), ones, ps[sub], false);
         }
       psum = ps[0] + ps[1];
     };
-    exps([&](float x) { return __builtin_fmaf(x, c, off); });
+    exps(off);
     if (__any(!(psum <= kLazyLimit))) {
       float tmax = sc[0][0];
 #pragma unroll
@@ -505,7 +505,13 @@ __global__ __launch_bounds__(64 * kFWaves, 1) void k_attn_mfma(dkv_bank bank, co
       const float noff = -mref * c;
       const bool far = is_far(noff);
       off = far || mnew == -INFINITY ? NAN : noff;
-      exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
+      if (__any(far)) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[sub][i] = far ? sc[sub][i] - mref : sc[sub][i];
+      }
+      exps(far ? 0.0f : noff);
     }
     lrun += psum;
 #pragma unroll

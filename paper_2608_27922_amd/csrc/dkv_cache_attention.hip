@@ -454,15 +454,15 @@ template <int D, int NSUB>
 __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t (*pb)[8], float c) {
   const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
   float psum = 0.0f;
-  auto exps = [&](auto exponent) __attribute__((always_inline)) {
+  auto exps = [&](float off) __attribute__((always_inline)) {
     psum = 0.0f;
 #pragma unroll
     for (int sub = 0; sub < NSUB; ++sub) {
       float ps = 0.0f;
 #pragma unroll
       for (int i = 0; i < 16; i += 2) {
-        const float p0 = __builtin_amdgcn_exp2f(exponent(sc[sub][i]));
-        const float p1 = __builtin_amdgcn_exp2f(exponent(sc[sub][i + 1]));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i], c, off));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[sub][i + 1], c, off));
         pb[sub][i >> 1] = pack_bf16x2(p0, p1);
         // row sum of the bf16 weights that are multiplied into O: their rounding (2^-8) enters
         // numerator and denominator alike.  It is a choice for speed: weights in two parts (two_parts) double
@@ -474,9 +474,9 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
       psum += ps;
     }
   };
-  exps([&](float x) { return __builtin_fmaf(x, c, r.off); });
+  exps(r.off);
   const bool over = !(psum <= kLazyLimit);
-  if (__any(over)) {
+  if (__builtin_expect(__any(over), 0)) {
     // only the rows concerned, so that a row's result does not depend on the rows beside it
     const bool raise = either_half(over);
     float tmax = sc[0][0];
@@ -497,7 +497,13 @@ __device__ __forceinline__ void softmax_update(Rows<D> &r, f32x16 *sc, uint32_t 
     const float noff = -mref * c;
     const bool far = is_far(noff);
     r.off = far || mnew == -INFINITY ? NAN : noff;
-    exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
+    if (__any(far)) {
+#pragma unroll
+      for (int sub = 0; sub < NSUB; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[sub][i] = far ? sc[sub][i] - mref : sc[sub][i];
+    }
+    exps(far ? 0.0f : noff);
   }
   r.lrun += psum;
 }
@@ -679,7 +685,7 @@ __device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const
 // Measured: bf16, 12 heads x 4,680 tokens over 15,600 keys, d = 128, 228 workgroups: 435 to 470 us on different cards, 960
 // to 1,030 TFLOP/s (a large library product: 1,175; the matrix pipe is busy 47% of the cycles of the 228 CUs,
 // the rest is a tile's softmax and its barrier: both waves of a SIMD come to them together).  8-bit pages, 12 x 1,560 over
-// 9,360 bank and 9,360 cache keys: 217 to 222 us with the joining of three splits, 820 TFLOP/s: the conversion of a tile
+// 9,360 bank and 9,360 cache keys: 213 to 222 us with the joining of three splits, 810 to 840 TFLOP/s: the conversion of a tile
 // runs between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
 // half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks of 478 to 777 tokens that see
 // 2,000 tokens each, 63 us, 393 TFLOP/s (13 us before the first product, 200 workgroups of 18 tiles).
@@ -997,17 +1003,17 @@ struct Wave16 {
     }
     uint32_t pb[4], pl[4];
     float psum = 0.0f;
-    auto exps = [&](auto exponent) __attribute__((always_inline)) {
+    auto exps = [&](float off) __attribute__((always_inline)) {
       psum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p0 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1)]));
-        const float p1 = __builtin_amdgcn_exp2f(exponent(sc[e >> 1][2 * (e & 1) + 1]));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1)], c, off));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1) + 1], c, off));
         two_parts(p0, p1, pb[e], pl[e]);
         psum += p0 + p1;
       }
     };
-    exps([&](float x) { return __builtin_fmaf(x, c, off); });
+    exps(off);
     const bool over = !(psum <= kLazyLimit);
     if (__any(over)) {  // as softmax_update
       int raise = over;
@@ -1027,7 +1033,13 @@ struct Wave16 {
       const float noff = -mref * c;
       const bool far = is_far(noff);
       off = far || mnew == -INFINITY ? NAN : noff;
-      exps([&](float x) { return far ? (x - mref) * c : __builtin_fmaf(x, c, noff); });
+      if (__any(far)) {
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sc[st][i] = far ? sc[st][i] - mref : sc[st][i];
+      }
+      exps(far ? 0.0f : noff);
     }
     lrun += psum;
     if (!whole) purge(vt, vis);
