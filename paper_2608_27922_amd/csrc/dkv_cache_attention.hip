@@ -689,8 +689,8 @@ __device__ __forceinline__ void load_q(bf16x8 *qf, const CacheQueries &qs, const
 // runs between two matrix blocks of the same wave, and two tiles ahead do not fit the registers.  d = 64 has
 // half the matrix work for the same softmax: 8-bit pages, 5 ragged chunks of 478 to 777 tokens that see
 // 2,000 tokens each, 63 us, 393 TFLOP/s (13 us before the first product, 200 workgroups of 18 tiles).
-// No vector register is spilled; 27 to 63 scalar ones are, into lanes of vector registers (kernel arguments, the plan of the
-// tiles and buffer descriptors that stay live over the loops).
+// No vector register is spilled but one in the path of raised references; 25 to 63 scalar ones are, into lanes of vector
+// registers (kernel arguments, the plan of the tiles and buffer descriptors that stay live over the loops).
 // Four waves a SIMD at d = 64 (128 registers) would spill 50 to 90 of them.
 // ---------------------------------------------------------------------------
 constexpr int kWWaves = 8, kWRows = 32 * kWWaves;
