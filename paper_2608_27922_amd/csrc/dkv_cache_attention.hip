@@ -1003,17 +1003,17 @@ struct Wave16 {
     }
     uint32_t pb[4], pl[4];
     float psum = 0.0f;
-    auto exps = [&](float off) __attribute__((always_inline)) {
+    auto exps = [&](float ref, float off) __attribute__((always_inline)) {
       psum = 0.0f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1)], c, off));
-        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1) + 1], c, off));
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1)] - ref, c, off));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[e >> 1][2 * (e & 1) + 1] - ref, c, off));
         two_parts(p0, p1, pb[e], pl[e]);
         psum += p0 + p1;
       }
     };
-    exps(off);
+    exps(0.0f, off);
     const bool over = !(psum <= kLazyLimit);
     if (__any(over)) {  // as softmax_update
       int raise = over;
@@ -1033,13 +1033,7 @@ struct Wave16 {
       const float noff = -mref * c;
       const bool far = is_far(noff);
       off = far || mnew == -INFINITY ? NAN : noff;
-      if (__any(far)) {
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sc[st][i] = far ? sc[st][i] - mref : sc[st][i];
-      }
-      exps(far ? 0.0f : noff);
+      exps(far ? mref : 0.0f, far ? 0.0f : noff);
     }
     lrun += psum;
     if (!whole) purge(vt, vis);
