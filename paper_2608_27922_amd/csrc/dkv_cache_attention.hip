@@ -928,7 +928,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // A pair of weights as two bf16 numbers each, their leading bits and the rest: 15 bits that the product with V keeps.  The
 // rest of a weight that is not zero is not zero either, so that its product with an infinity is that infinity.  With 16
 // rows a wave the matrix pipe has the time (error 2.4 -> 1.7e-3 as at softmax_update; single tokens of 64 sequences over
-// 8 bits 166 -> 168 us, over 4 bits 116 -> 123, over bf16 289 -> 290).
+// 8 bits 166 -> 168 us, over 4 bits 116 -> 122, over bf16 289 -> 290; at d = 64, where the vector work bounds quantised
+// pages, 4 bits 73 -> 80 and 20 sequences of 8 bits 57 -> 61).
 __device__ __forceinline__ void two_parts(float p0, float p1, uint32_t &lead, uint32_t &rest) {
   const uint32_t a = __float_as_uint(p0), b = __float_as_uint(p1);
   lead = __builtin_amdgcn_perm(b, a, 0x07060302u);
